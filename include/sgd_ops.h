@@ -1,6 +1,8 @@
 /*
- * sgd_ops.h -- single-kernel entry points of libsgd, for kernel-level parity tests and
- * microbenchmarks.  They run exactly the kernels that sgd_denoise_step launches.
+ * sgd_ops.h -- single-kernel entry points of libsgd.  The first part, up to the microscaled rows, is
+ * for kernel-level parity tests and microbenchmarks: exactly the kernels that sgd_denoise_step launches.  The
+ * second part are operators of units beyond it: rows in 8 and 4 bits and their products, rotary positions,
+ * attention over key intervals.
  *
  * Conventions as in sgd.h: int status (SGD_OK or SGD_E_*), device pointers, enqueue on
  * hip_stream without synchronising, caller-owned buffers, no allocation.
@@ -116,6 +118,111 @@ int sgd_op_group_norm_silu(int32_t in_dtype, const void* x, void* y, int32_t B, 
  * Cin % 64 == 0, N % 4 == 0.  tile: 0 auto, or 2, 4, 5, 6, 7 (numbered as for sgd_op_linear). */
 int sgd_op_conv3x3(const void* A, const void* W, const float* bias, const float* rowbias, int32_t side, void* out,
                    float* h, int32_t M, int32_t N, int32_t Cin, int32_t tile, void* hip_stream);
+
+/* ------------------------------------------------------------ microscaled rows
+ * Rows in 8 or 4 bits with one power-of-two scale per 32 columns (the OCP Microscaling formats):
+ *   codes   SGD_MX_FP8: e4m3, one byte a value, K bytes a row; SGD_MX_FP4: e2m1, K / 2 bytes a row, the
+ *           even column in the low four bits.  Rows are compact (no row stride).
+ *   scales  one byte per row and 32 columns, 2^(byte - 127), 255: NaN; in chunks of eight blocks,
+ *           [ceil(K / 256)][rows][8]: byte (c, r, i) is block 8 c + i of row r.  Bytes past the last
+ *           block (K % 256 != 0) are written as 0; whoever makes scales must not leave 255 there.
+ * Quantisation of a block: scale 2^(floor(log2(max |x|)) - e), e = 8 (e4m3) or 2 (e2m1), not below 2^-127; each
+ * x / scale rounded to nearest, ties to even, saturating at 448 or 6 (at most an eighth, or a quarter,
+ * off the block's largest values).  A block that holds an infinity or a NaN gets scale 255.
+ * K % 32 == 0, codes 16-byte and scales 8-byte aligned. */
+enum sgd_mx_format { SGD_MX_FP8 = 0, SGD_MX_FP4 = 1 };
+
+/* Bytes of the codes and scales of `rows` rows of K columns. */
+int sgd_op_mx_bytes(int32_t format, int64_t rows, int32_t K, size_t* codes, size_t* scales);
+
+/* x [rows x K] of dtype, rows ldx elements apart (16-byte aligned rows), to codes and scales;
+ * rows * K < 2^34. */
+int sgd_op_mx_quantize(int32_t format, int32_t dtype, const void* x, int64_t ldx, int32_t rows, int32_t K,
+                       void* codes, uint8_t* scales, void* hip_stream);
+/* The values back: out [rows x K] of dtype (exact in fp32; in bf16 but for results past its range). */
+int sgd_op_mx_dequantize(int32_t format, const void* codes, const uint8_t* scales, int32_t rows, int32_t K,
+                         int32_t dtype, void* out, int64_t ldo, void* hip_stream);
+
+/* sgd_op_linear on microscaled rows: out = act(A W^T + bias) with A [M x K] in a_format and W [N x K] (gated:
+ * [2N x K] = [W_gate; W_up]) in SGD_MX_FP4.  out_dtype SGD_BF16, or SGD_F32 (ungated, act SGD_ACT_NONE); rows of
+ * out ldo elements apart.  Products are exact and summed in fp32; with A in e4m3 the matrix cores align 64
+ * products to their largest and drop what lies about 16 bits below it (up to 5e-5 of the result's size
+ * where A's codes span the format's whole range).  tile: 0 auto, 1..6 block tiles (256x256, 256x128, 128x256,
+ * 128x128, 128x64, 64x64), 7 the kernel for up to 16 rows.  N % 4 == 0 (gated: N % 32 == 0, and on a fixed
+ * tile 2N a multiple of its width), bias 16-byte, out 8-byte (fp32: 16-byte) aligned, ldo % 4 == 0, each
+ * operand's scales and W's codes below 4 GiB. */
+int sgd_op_linear_mx(int32_t a_format, const void* a_codes, const uint8_t* a_scales, const void* w_codes,
+                     const uint8_t* w_scales, const float* bias, int32_t out_dtype, void* out, int64_t ldo,
+                     int32_t M, int32_t N, int32_t K, int32_t act, int32_t gated, int32_t tile, void* hip_stream);
+
+/* The pre-norm that adds a branch's output to the stream and writes 8- or 4-bit rows: h = x + add (fp32
+ * sum, held in x's type), xo = h, codes and scales = h / sqrt(mean(h^2) + eps) w.  x, xo [M x d] of x_dtype
+ * (xo may be x), add [M x d] of add_dtype or NULL (then h = x and xo is not written; it may be NULL).  The
+ * norm is evaluated in fp64 and rounded once.  d % 32 == 0, d <= 8192; x, add, xo, w 16-byte aligned, none
+ * of them overlapping codes or scales. */
+int sgd_op_norm_add_mx(int32_t format, int32_t x_dtype, const void* x, int32_t add_dtype, const void* add, void* xo,
+                       const float* w, float eps, int32_t M, int32_t d, void* codes, uint8_t* scales, void* hip_stream);
+
+/* ------------------------------------------------------------ rotary positions */
+
+/* How the rotation speeds of a head's pairs are scaled for contexts longer than the model's own.
+ *   SGD_ROPE_PLAIN   base^(-2 i / rot) radians a token for pair i < rot / 2
+ *   SGD_ROPE_LINEAR  all of them divided by factor
+ *   SGD_ROPE_BASE    base factor^(rot / (rot - 2)) in place of base (the slowest pair is divided by factor,
+ *                    the fastest kept); rot > 2
+ *   SGD_ROPE_PARTS   pairs of more than `high` turns over `context` tokens kept, those of fewer than
+ *                    `low` divided by factor, in between mixed linearly in the number of turns; the rotated
+ *                    dims are also to be multiplied by 0.1 ln(factor) + 1 (the magnitude returned) */
+enum sgd_rope_scaling { SGD_ROPE_PLAIN = 0, SGD_ROPE_LINEAR = 1, SGD_ROPE_BASE = 2, SGD_ROPE_PARTS = 3 };
+typedef struct {
+    double base;      /* 10000 in the LLaDA attention; > 0 */
+    int32_t scaling;  /* sgd_rope_scaling */
+    double factor;    /* >= 1; not read for SGD_ROPE_PLAIN */
+    double context;   /* SGD_ROPE_PARTS: the model's own context, > 0 */
+    double low, high; /* SGD_ROPE_PARTS: 0 <= low < high, usually 1 and 32 */
+} sgd_rope_params;
+/* Host only: turns per token of the rot / 2 pairs (turns: host [rot / 2]) and the magnitude. */
+int sgd_rope_turns(const sgd_rope_params* params, int32_t rot, double* turns, double* magnitude);
+
+/* Rotates dims [0, rot) of every head of T tokens by their position and copies the others: x, out [T, H, dh] of
+ * dtype, last dim contiguous, token and head strides in elements (out may be x with the same strides; no
+ * other overlap).  Pair p is dims (p, p + rot / 2), or with interleaved != 0 (2 p, 2 p + 1); it turns by pos[t]
+ * turns[p] (device fp64 [rot / 2], as from sgd_rope_turns, taken in fp64) and is multiplied by magnitude;
+ * inverse != 0 turns back (and multiplies: the transpose, which is the gradient).  pos device int32 [T], or NULL:
+ * token t is at position t.  rot even, 2 <= rot <= dh <= 256, H <= 65535. */
+int sgd_op_rotary(int32_t dtype, const void* x, int64_t x_token, int64_t x_head, void* out, int64_t out_token,
+                  int64_t out_head, int32_t T, int32_t H, int32_t dh, int32_t rot, int32_t interleaved, const int32_t* pos,
+                  const double* turns, float magnitude, int32_t inverse, void* hip_stream);
+
+/* ------------------------------------------------------------ attention over key intervals */
+
+/* One call of sgd_op_attention_ranges.  Tensors are rows of dh contiguous values with strides
+ * (batch, token, head) in elements: q, o [B, nq, H, dh], k, v [B, nk, Hk, dh]; H / Hk query heads share a key
+ * head (query heads h G .. h G + G - 1 belong to key head h, G = H / Hk).
+ *   ranges  device int32 [B, nq, 2]: query i of sample b sees the keys lo <= j < hi (clipped to 0 <= j < nk); where
+ *           lo >= hi the output is zero.  Packed documents, prefixes, causal order, padding, windows.
+ *   scale   factor of the scores (> 0; 0 selects 1 / sqrt(dh))
+ *   cap     0, or > 0: scores become cap tanh(score / cap)
+ *   slopes  NULL, or device fp32 [H]: slope |pos - j| is subtracted from the (capped) score of key j
+ *   pos     device int32 [B, nq]: the queries' key positions, for slopes; NULL: i + nk - nq
+ * 8 <= dh <= 128, dh % 8 == 0; q, k, v rows 16-byte aligned (strides of 8 bf16 or 4 fp32 values), o 8-byte
+ * (fp32: 16-byte); token strides of k and v at least dh and below 2^24.  Keys and values that no query sees are
+ * not used, whatever they hold; infinities and NaN reach only the queries that see them. */
+typedef struct {
+    const void *q, *k, *v;
+    void* o;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+    const int32_t* ranges;
+    const int32_t* pos;
+    const float* slopes;
+    int32_t B, H, Hk, dh, nq, nk;
+    float scale, cap;
+} sgd_range_attention;
+/* Device workspace (16-byte aligned) of a call, 0 for most: with few query rows the keys are split between
+ * workgroups, whose results meet there.  Nothing in it needs to start at any value. */
+int sgd_op_attention_ranges_bytes(int32_t dtype, const sgd_range_attention* call, size_t* bytes);
+int sgd_op_attention_ranges(int32_t dtype, const sgd_range_attention* call, void* workspace, size_t workspace_bytes,
+                            void* hip_stream);
 
 #ifdef __cplusplus
 }

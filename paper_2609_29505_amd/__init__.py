@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     op_linear, op_linear_split, op_attention, op_norm, op_norm_fold, op_frozen_run, op_heads, op_residual,
     op_adaln_mod,
     op_group_norm_silu, op_conv3x3,
+    SGD_MX, SGD_ROPE, MxTensor, op_mx_quantize, op_mx_dequantize, op_linear_mx, op_norm_add_mx, rope_turns, op_rotary,
+    op_attention_ranges,
 )

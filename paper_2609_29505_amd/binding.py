@@ -17,6 +17,8 @@ lib_path = os.path.join(_PKG, "lib", "libsgd.so")
 SGD_F32, SGD_BF16 = 0, 1
 SGD_ARCH = {"tiny": 0, "llada": 1, "dit": 2, "uvit": 3, "sdxl": 4, "sdxl_unet": 5}
 SGD_UNIT = {"block": 0, "branch": 1}
+SGD_MX = {"fp8": 0, "fp4": 1}
+SGD_ROPE = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 SGD_RULE = {"scr_frob": 0, "random": 1, "depth": 2, "frob": 3, "spectral": 4, "stable_rank": 5,
             "frob_srank": 6, "raw_scr": 7}
 SGD_ROLE = {"q": 0, "k": 1, "v": 2, "o": 3, "xq": 4, "xk": 5, "xv": 6, "xo": 7, "w1": 8, "w2": 9, "conv": 10}
@@ -83,6 +85,19 @@ class sgd_step_args(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+class sgd_rope_params(C.Structure):
+    _fields_ = [("base", C.c_double), ("scaling", C.c_int32), ("factor", C.c_double), ("context", C.c_double),
+                ("low", C.c_double), ("high", C.c_double)]
+
+
+class sgd_range_attention(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("o", C.c_void_p),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("o_stride", C.c_int64 * 3), ("ranges", C.c_void_p), ("pos", C.c_void_p), ("slopes", C.c_void_p),
+                ("B", C.c_int32), ("H", C.c_int32), ("Hk", C.c_int32), ("dh", C.c_int32), ("nq", C.c_int32),
+                ("nk", C.c_int32), ("scale", C.c_float), ("cap", C.c_float)]
+
+
 # ------------------------------------------------------------------ library
 
 _lib = None
@@ -97,7 +112,9 @@ EXPORTS = ["sgd_last_error", "sgd_version", "sgd_s_min_default", "sgd_budget_lay
            "sgd_profile_begin", "sgd_profile_end", "sgd_op_linear", "sgd_op_linear_split",
            "sgd_op_linear_split_tile", "sgd_op_attention", "sgd_op_norm", "sgd_op_norm_fold",
            "sgd_op_frozen_run", "sgd_op_heads", "sgd_op_residual", "sgd_op_adaln_mod", "sgd_op_group_norm_silu",
-           "sgd_op_group_norm_scratch_bytes", "sgd_op_conv3x3"]
+           "sgd_op_group_norm_scratch_bytes", "sgd_op_conv3x3", "sgd_op_mx_bytes", "sgd_op_mx_quantize",
+           "sgd_op_mx_dequantize", "sgd_op_linear_mx", "sgd_op_norm_add_mx", "sgd_rope_turns", "sgd_op_rotary",
+           "sgd_op_attention_ranges_bytes", "sgd_op_attention_ranges"]
 
 
 def lib() -> C.CDLL:
@@ -157,6 +174,15 @@ def lib() -> C.CDLL:
             "sgd_op_group_norm_scratch_bytes": [i32, i32, i32, C.POINTER(C.c_size_t)],
             "sgd_op_group_norm_silu": [i32, vp, vp, i32, i32, i32, i32, C.c_float, vp, vp, vp, C.c_size_t, vp],
             "sgd_op_conv3x3": [vp, vp, vp, vp, i32, vp, vp, i32, i32, i32, i32, vp],
+            "sgd_op_mx_bytes": [i32, i64, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)],
+            "sgd_op_mx_quantize": [i32, i32, vp, i64, i32, i32, vp, vp, vp],
+            "sgd_op_mx_dequantize": [i32, vp, vp, i32, i32, i32, vp, i64, vp],
+            "sgd_op_linear_mx": [i32, vp, vp, vp, vp, vp, i32, vp, i64, i32, i32, i32, i32, i32, i32, vp],
+            "sgd_op_norm_add_mx": [i32, i32, vp, i32, vp, vp, vp, C.c_float, i32, i32, vp, vp, vp],
+            "sgd_rope_turns": [C.POINTER(sgd_rope_params), i32, C.POINTER(C.c_double), C.POINTER(C.c_double)],
+            "sgd_op_rotary": [i32, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, i32, vp, vp, C.c_float, i32, vp],
+            "sgd_op_attention_ranges_bytes": [i32, C.POINTER(sgd_range_attention), C.POINTER(C.c_size_t)],
+            "sgd_op_attention_ranges": [i32, C.POINTER(sgd_range_attention), vp, C.c_size_t, vp],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -438,6 +464,158 @@ def op_conv3x3(A, W, side, out=None, h=None, bias=None, rowbias=None, tile=0, st
 def op_frozen_run(h, deltas, stream=None) -> None:
     arr = (C.c_void_p * len(deltas))(*[t.data_ptr() for t in deltas])
     _check(lib().sgd_op_frozen_run(_p(h), arr, len(deltas), h.numel(), C.c_void_p(_stream_ptr(stream))))
+
+
+def _expect(t, name, dtype, shape, contiguous=True) -> None:
+    """The tensors of a call agree with each other (the library sees pointers only)."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or (contiguous and not t.is_contiguous()):
+        raise ValueError(f"{name}: expected a {'contiguous ' if contiguous else ''}device tensor {dtype} {tuple(shape)}, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+
+
+def _one_device(*tensors) -> None:
+    import torch
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor on {t.device}, the current device is {torch.cuda.current_device()}")
+
+
+class MxTensor:
+    """Microscaled rows (see sgd_ops.h): ``fmt`` "fp8" or "fp4", ``codes`` uint8 [rows, K or K / 2], ``scales`` uint8
+    [ceil(K / 256), rows, 8]."""
+
+    def __init__(self, fmt: str, codes, scales):
+        import torch
+        self.fmt, self.codes, self.scales = fmt, codes, scales
+        if codes.dim() != 2:
+            raise ValueError("codes are [rows, bytes of a row]")
+        self.rows, self.K = codes.shape[0], codes.shape[1] * (1 if SGD_MX[fmt] == 0 else 2)
+        _expect(codes, "codes", torch.uint8, codes.shape)
+        _expect(scales, "scales", torch.uint8, (-(-self.K // 256), self.rows, 8))
+
+    @classmethod
+    def empty(cls, fmt: str, rows: int, K: int) -> "MxTensor":
+        import torch
+        nc, ns = C.c_size_t(), C.c_size_t()
+        _check(lib().sgd_op_mx_bytes(SGD_MX[fmt], rows, K, C.byref(nc), C.byref(ns)))
+        return cls(fmt, torch.empty(rows, nc.value // rows, dtype=torch.uint8, device="cuda"),
+                   torch.empty(-(-K // 256), rows, 8, dtype=torch.uint8, device="cuda"))
+
+
+def _rows2d(t, name, rows, K) -> int:
+    """Row stride of a 2-D device tensor with contiguous rows."""
+    if not t.is_cuda or tuple(t.shape) != (rows, K) or (K > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected a device tensor {(rows, K)} with contiguous rows, got {tuple(t.shape)}")
+    return t.stride(0) if rows > 1 else K
+
+
+def op_mx_quantize(x, mx: MxTensor, stream=None) -> None:
+    """x [rows, K] (bf16 or fp32, rows strided) into ``mx``."""
+    _one_device(x, mx.codes, mx.scales)
+    ld = _rows2d(x, "x", mx.rows, mx.K)
+    _check(lib().sgd_op_mx_quantize(SGD_MX[mx.fmt], _dtype_code(x), _p(x), ld, mx.rows, mx.K, _p(mx.codes),
+                                    _p(mx.scales), C.c_void_p(_stream_ptr(stream))))
+
+
+def op_mx_dequantize(mx: MxTensor, out, stream=None) -> None:
+    """The values of ``mx`` into out [rows, K] (bf16 or fp32, rows strided)."""
+    _one_device(out, mx.codes, mx.scales)
+    ld = _rows2d(out, "out", mx.rows, mx.K)
+    _check(lib().sgd_op_mx_dequantize(SGD_MX[mx.fmt], _p(mx.codes), _p(mx.scales), mx.rows, mx.K, _dtype_code(out),
+                                      _p(out), ld, C.c_void_p(_stream_ptr(stream))))
+
+
+def op_linear_mx(A: MxTensor, W: MxTensor, out, bias=None, act=0, gated=False, tile=0, stream=None) -> None:
+    """out [M, N] = act(A W^T + bias); gated: W = [W_gate; W_up] with 2 N rows.  W in "fp4"."""
+    import torch
+    _one_device(A.codes, A.scales, W.codes, W.scales, out, bias)
+    n = W.rows // 2 if gated else W.rows
+    if W.fmt != "fp4" or W.K != A.K or (gated and W.rows % 2):
+        raise ValueError(f"W must be fp4 rows of A's {A.K} columns (gated: an even number of them)")
+    ldo = _rows2d(out, "out", A.rows, n)
+    if bias is not None:
+        _expect(bias, "bias", torch.float32, (W.rows,))
+    _check(lib().sgd_op_linear_mx(SGD_MX[A.fmt], _p(A.codes), _p(A.scales), _p(W.codes), _p(W.scales), _p(bias),
+                                  _dtype_code(out), _p(out), ldo, A.rows, n, A.K, act, int(gated), tile,
+                                  C.c_void_p(_stream_ptr(stream))))
+
+
+def op_norm_add_mx(x, w, mx: MxTensor, eps, add=None, out=None, stream=None) -> None:
+    """h = x + add, out = h (None: written back to x), mx = h / rms(h) * w; without ``add`` h = x and nothing but
+    ``mx`` is written."""
+    import torch
+    xo = None if add is None else x if out is None else out
+    _one_device(x, w, mx.codes, mx.scales, add, xo)
+    _expect(x, "x", x.dtype, (mx.rows, mx.K))
+    _expect(w, "w", torch.float32, (mx.K,))
+    if add is not None:
+        _expect(add, "add", add.dtype, (mx.rows, mx.K))
+        _expect(xo, "out", x.dtype, (mx.rows, mx.K))
+    elif out is not None:
+        raise ValueError("without add there is no sum to write to out")
+    _check(lib().sgd_op_norm_add_mx(SGD_MX[mx.fmt], _dtype_code(x), _p(x), 0 if add is None else _dtype_code(add), _p(add),
+                                    _p(xo), _p(w), eps, mx.rows, mx.K, _p(mx.codes), _p(mx.scales),
+                                    C.c_void_p(_stream_ptr(stream))))
+
+
+def rope_turns(rot, base=10000.0, scaling="plain", factor=1.0, context=0.0, low=1.0, high=32.0):
+    """(turns per token of the rot / 2 pairs as a float64 array, magnitude); see sgd_rope_turns."""
+    p = sgd_rope_params(base, SGD_ROPE[scaling], factor, context, low, high)
+    out = np.zeros(max(int(rot), 2) // 2, np.float64)
+    mag = C.c_double()
+    _check(lib().sgd_rope_turns(C.byref(p), rot, out.ctypes.data_as(C.POINTER(C.c_double)), C.byref(mag)))
+    return out, float(mag.value)
+
+
+def op_rotary(x, out, turns, pos=None, interleaved=False, magnitude=1.0, inverse=False, stream=None) -> None:
+    """Rotates the first 2 len(turns) dims of x [T, H, dh] by ``pos`` (int32 [T]; None: the token's index) into
+    ``out`` (may be x); ``turns``: float64 device tensor, as from rope_turns."""
+    import torch
+    _one_device(x, out, turns, pos)
+    if x.dim() != 3 or x.stride(2) != 1 or out.stride(-1) != 1:
+        raise ValueError("x and out are [T, H, dh] with contiguous heads")
+    T, H, dh = x.shape
+    _expect(out, "out", x.dtype, x.shape, contiguous=False)
+    _expect(turns, "turns", torch.float64, (turns.numel(),))
+    if pos is not None:
+        _expect(pos, "pos", torch.int32, (T,))
+    _check(lib().sgd_op_rotary(_dtype_code(x), _p(x), x.stride(0), x.stride(1), _p(out), out.stride(0), out.stride(1),
+                               T, H, dh, 2 * turns.numel(), int(interleaved), _p(pos), _p(turns), magnitude,
+                               int(inverse), C.c_void_p(_stream_ptr(stream))))
+
+
+def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, pos=None, workspace=None, stream=None) -> None:
+    """Attention of q [B, nq, H, dh] over k, v [B, nk, Hk, dh] into o [B, nq, H, dh] (contiguous heads, other
+    strides free), query (b, i) seeing the keys ranges[b, i] = (lo, hi) (int32 [B, nq, 2]); see sgd_ops.h.
+    ``workspace``: a uint8 device tensor for the calls that need one (None: allocated here)."""
+    import torch
+    _one_device(q, k, v, o, ranges, slopes, pos, workspace)
+    B, nq, H, dh = q.shape
+    nk, Hk = k.shape[1], k.shape[2]
+    _expect(k, "k", q.dtype, (B, nk, Hk, dh), contiguous=False)
+    _expect(v, "v", q.dtype, (B, nk, Hk, dh), contiguous=False)
+    _expect(o, "o", q.dtype, (B, nq, H, dh), contiguous=False)
+    _expect(ranges, "ranges", torch.int32, (B, nq, 2))
+    if any(t.stride(3) != 1 for t in (q, k, v, o)):
+        raise ValueError("heads must be contiguous")
+    if slopes is not None:
+        _expect(slopes, "slopes", torch.float32, (H,))
+    if pos is not None:
+        _expect(pos, "pos", torch.int32, (B, nq))
+    st = [(C.c_int64 * 3)(*t.stride()[:3]) for t in (q, k, v, o)]
+    c = sgd_range_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), *st, ranges.data_ptr(),
+                            pos.data_ptr() if pos is not None else None,
+                            slopes.data_ptr() if slopes is not None else None, B, H, Hk, dh, nq, nk,
+                            0.0 if scale is None else scale, cap)
+    dt = _dtype_code(q)
+    nb = C.c_size_t()
+    _check(lib().sgd_op_attention_ranges_bytes(dt, C.byref(c), C.byref(nb)))
+    sp = C.c_void_p(_stream_ptr(stream))
+    if nb.value and workspace is None:
+        workspace = _workspace(nb.value)
+        if stream is not None:
+            workspace.record_stream(stream)  # it may be freed here while the call is still to run there
+    _check(lib().sgd_op_attention_ranges(dt, C.byref(c), _p(workspace), workspace.numel() if workspace is not None else 0, sp))
 
 
 # ------------------------------------------------------------------ model

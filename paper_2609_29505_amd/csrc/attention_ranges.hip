@@ -1,0 +1,716 @@
+// Attention in which every query sees an interval of keys: o = sum_j p_j v_j / sum_j p_j over lo <= j < hi,
+// p_j = exp(f(q . k_j scale) - slope |pos - j|), f(x) = x or cap tanh(x / cap).  Documents packed into one
+// sequence, prefixes, causal order, padding and windows are all such intervals; a query that sees nothing
+// gets zeros.  One pass over the keys with a running maximum and sum.
+//
+// Rows of a key head are its queries times the G query heads that share it (row = query G + head), so that
+// grouped heads read their keys and values once.  A wave owns 32 rows and computes S^T = K Q^T, as in
+// attention.hip: one lane holds one row's scores, and P^T is the right operand of O^T += V^T P^T as it is.  Keys
+// and values are read from their token-major rows (any strides): the matrix instruction wants eight keys
+// of one dim in a lane, which the transposing LDS read (ds_read_b64_tr_b16) gives from rows stored as they are.
+//
+// Blocks of 64 keys outside every row's interval are skipped, blocks inside all of a wave's intervals
+// are not masked.  A key's value may be infinite or NaN where some rows do not see it (0 x inf is NaN in the
+// matrix instruction): blocks that are not wholly visible are looked over for such values, which are
+// taken out of the block and added one key at a time to the rows that see them.
+//
+// Few rows: the keys of a row block are split between workgroups (splits), whose (maximum, sum, O) meet
+// in the workspace; with up to 32 rows the four waves of a workgroup also take different keys.
+#include <float.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "gemm_common.h"
+#include "kernels.h"
+#include "tile_order.h"
+
+namespace sgd {
+
+namespace {
+constexpr float kLog2e = 1.44269504088896340736f;
+// lazy rescaling: the running maximum is raised only when a block's exceeds it by 2^8 (attention.hip)
+constexpr float kSlack = 8.0f;
+
+__device__ __forceinline__ float half_max(float v) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// What a lane knows of its row
+struct Row {
+    int lo, hi;      // visible keys; lo = hi: none
+    int pos;         // the query's key position
+    float slope;     // distance bias, log2 domain
+    float c0, c1;    // scores: raw c0 (no cap), or c0 (1 - 2 / (1 + 2^(raw c1)))
+};
+
+// Row r of key head hk (nr rows), sample b; rows past the last see nothing
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ Row row_info(const RangeAttnArgs& a, int b, int hk, int r, int nr, int G, int& i, int& h) {
+    const int rc = min(r, nr - 1);
+    i = rc / G;
+    h = hk * G + (rc - i * G);
+    Row w;
+    const long at = (long)b * a.nq + i;
+    w.lo = max(a.ranges[2 * at], 0);
+    w.hi = min(a.ranges[2 * at + 1], a.nk);
+    if (r >= nr || w.lo >= w.hi) w.lo = w.hi = 0;
+    w.pos = BIAS ? (a.pos ? a.pos[at] : i + a.nk - a.nq) : 0;
+    w.slope = BIAS ? a.slopes[h] * kLog2e : 0.f;
+    w.c0 = (CAP ? a.cap : a.scale) * kLog2e;
+    w.c1 = CAP ? 2.0f * a.scale * kLog2e / a.cap : 0.f;
+    return w;
+}
+
+// Union and intersection of the wave's non-empty intervals
+struct Span { int lo, hi, ilo, ihi; };
+__device__ __forceinline__ Span wave_span(const Row& w) {
+    const bool some = w.lo < w.hi;
+    Span s{some ? w.lo : INT32_MAX, some ? w.hi : 0, some ? w.lo : 0, some ? w.hi : INT32_MAX};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s.lo = min(s.lo, __shfl_xor(s.lo, o, 64));
+        s.hi = max(s.hi, __shfl_xor(s.hi, o, 64));
+        s.ilo = max(s.ilo, __shfl_xor(s.ilo, o, 64));
+        s.ihi = min(s.ihi, __shfl_xor(s.ihi, o, 64));
+    }
+    s.lo = __builtin_amdgcn_readfirstlane(s.lo);
+    s.hi = __builtin_amdgcn_readfirstlane(s.hi);
+    s.ilo = __builtin_amdgcn_readfirstlane(s.ilo);
+    s.ihi = __builtin_amdgcn_readfirstlane(s.ihi);
+    return s;
+}
+
+// Key (relative to the lane's first) of score register r of 32-key group t
+__device__ __forceinline__ constexpr int key_of(int t, int r) { return t * 32 + (r >> 2) * 8 + (r & 3); }
+
+// One block's softmax: raw scores s (key of register (t, r): key0 + key_of(t, r)) become probabilities.  The
+// running maximum m (log2 domain; -FLT_MAX before the first visible key, so that no difference is NaN) and
+// the lane's partial sum go on; returns the factor for what was accumulated before.
+template <bool CAP, bool BIAS, int NS>
+__device__ __forceinline__ float softmax_block(f32x16 (&s)[NS], const Row& w, int key0, bool masked, float& m, float& lsum) {
+    constexpr bool LATE = !CAP && !BIAS;  // the plain scale is folded into the exponent
+    if constexpr (!LATE) {
+        const float d0 = BIAS ? (float)(w.pos - key0) : 0.f;
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float x = s[t][r];
+                if constexpr (CAP) x = w.c0 - 2.0f * w.c0 * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * w.c1));
+                else x *= w.c0;
+                if constexpr (BIAS) x = fmaf(-w.slope, fabsf(d0 - (float)key_of(t, r)), x);
+                s[t][r] = x;
+            }
+    }
+    if (masked) {
+        const unsigned a = (unsigned)(w.lo - key0), n = (unsigned)(w.hi - w.lo);
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((unsigned)key_of(t, r) - a >= n) s[t][r] = -INFINITY;
+    }
+    float bm = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, s[t][r]);
+    bm = half_max(bm);
+    if constexpr (LATE) bm *= w.c0;
+    float alpha = 1.0f;
+    if (__builtin_amdgcn_ballot_w64(bm > m + kSlack)) {
+        const float mn = fmaxf(m, bm);
+        alpha = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        lsum *= alpha;
+    }
+    float ps = 0.f;
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float p = __builtin_amdgcn_exp2f(LATE ? fmaf(s[t][r], w.c0, -m) : s[t][r] - m);
+            s[t][r] = p;
+            ps += p;
+        }
+    lsum += ps;
+    return alpha;
+}
+
+// Where a row's partial result goes: [split][b Hk + hk][row][dh + 4] fp32: O, then the maximum and the sum
+__device__ __forceinline__ float* partial_row(const RangeAttnArgs& a, int split, int bh, int r) {
+    const long nr = (long)a.nq * (a.H / a.Hk);
+    return (float*)a.work + (((long)split * a.B * a.Hk + bh) * nr + r) * (a.dh + 4);
+}
+
+// A lane's O^T (dims dt 32 + 8 (r / 4) + 4 half + r % 4 of its row), maximum and whole sum: divided and
+// stored, or left for the join
+template <int DT, typename T>
+__device__ __forceinline__ void finish(const RangeAttnArgs& a, const f32x16 (&o)[DT], const Row& w, float m, float l, int split,
+                                       int b, int hk, int bh, int r, int nr, int i, int h, int half) {
+    if (r >= nr) return;
+    const bool some = w.lo < w.hi;
+    if (a.splits > 1) {
+        float* const p = partial_row(a, split, bh, r);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int d = dt * 32 + g * 8 + half * 4;
+                if (d < a.dh) *(f32x4*)(p + d) = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+            }
+        if (half == 0) {
+            p[a.dh] = m;
+            p[a.dh + 1] = some ? l : -1.0f;  // -1: the row sees nothing
+        }
+        return;
+    }
+    T* const dst = (T*)a.o + b * a.os[0] + i * a.os[1] + h * a.os[2];
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = dt * 32 + g * 8 + half * 4;
+            if (d >= a.dh) continue;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = some ? o[dt][4 * g + e] * inv : 0.f;
+            if constexpr (sizeof(T) == 2) store_bf16x4((bf16*)dst + d, v);
+            else *(f32x4*)(dst + d) = f32x4{v[0], v[1], v[2], v[3]};
+        }
+}
+
+// Bits of a pair of bf16 values: 0x8000 in each half that holds an infinity or a NaN
+__device__ __forceinline__ uint32_t odd_pair(uint32_t x) { return ((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+
+// Looks over 16 bytes of values in LDS and clears infinities and NaN there; whether there were any
+__device__ __forceinline__ bool clear_odd(char* p) {
+    u32x4 x = *(const u32x4*)p;
+    uint32_t odd = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= odd_pair(x[e]);
+    if (odd) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] &= ~((odd_pair(x[e]) >> 15) * 0xFFFFu);
+        *(u32x4*)p = x;
+    }
+    return odd != 0;
+}
+
+// The infinities and NaN that were cleared from a block, added to the rows that see them: keys [j0, j1), read
+// again from memory one at a time (V: key 0, ts elements a key)
+template <int DT, typename T>
+__device__ __forceinline__ void add_odd(f32x16 (&o)[DT], const Row& w, const T* V, long ts, int j0, int j1, int dh, int half) {
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+        const bool see = j >= w.lo && j < w.hi;
+        const T* const p = V + j * ts + half * 4;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                asm volatile("" : "+s"(dh));  // sixteen addresses kept over the main loop would spill
+                const int d = min(dt * 32 + g * 8, dh - 8);  // what lies past dh is not stored
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = ElemIO<T>::load(p + d + e);
+                    o[dt][4 * g + e] += see && !(fabsf(v) <= FLT_MAX) ? v : 0.f;
+                }
+                __builtin_amdgcn_sched_barrier(0);  // a rare path: it takes no registers from the others
+            }
+    }
+}
+
+// K and V tiles in LDS, bf16: rows of P bytes, 16-byte chunks swizzled
+template <int DH> struct Tile {
+    static constexpr int P = DH <= 64 ? 128 : 256, CH = P / 16;
+    static constexpr int KS = DH / 16, DT = DH / 32;
+    // fragment reads of 16 consecutive keys cover the 64 banks once
+    __device__ static __forceinline__ int kpos(int key, int c) { return P == 256 ? c ^ (key & 15) : c ^ ((key >> 1) & 7); }
+    // a transposing read takes 64 bytes of each of four consecutive keys: in different banks
+    __device__ static __forceinline__ int vpos(int key, int c) { return P == 256 ? c ^ ((key & 3) << 2) : c ^ (((key >> 1) & 1) << 2); }
+};
+
+typedef __bf16 __attribute__((ext_vector_type(4))) tr4;
+__device__ __forceinline__ bf16x4 read_tr(const char* p) {
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((tr4 __attribute__((address_space(3)))*)(__attribute__((address_space(3))) char*)p));
+}
+
+// V^T fragment of 16-key group k16 (keys 16 k16 + 4 half + 0..3 and + 8), dims 32 dt + lane % 32; at: the lane's
+// place in its tile for group 0, dims 0
+template <int DH>
+struct VRead {
+    const char* p[Tile<DH>::DT];
+    __device__ __forceinline__ VRead(const char* tile, int lane) {
+        const int half = lane >> 5, i = lane & 15, key = half * 4 + (i >> 2);
+#pragma unroll
+        for (int dt = 0; dt < Tile<DH>::DT; ++dt) {
+            const int d = dt * 32 + ((lane >> 4) & 1) * 16 + (i & 3) * 4;
+            p[dt] = tile + key * Tile<DH>::P + Tile<DH>::vpos(key, d >> 3) * 16 + (d & 4) * 2;
+        }
+    }
+    // the swizzle depends on the key's last two bits only: steps of eight keys keep it
+    __device__ __forceinline__ bf16x8 frag(int off, int dt, int k16) const {
+        const bf16x4 a = read_tr(p[dt] + off + k16 * 16 * Tile<DH>::P), b = read_tr(p[dt] + off + (k16 * 16 + 8) * Tile<DH>::P);
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// O^T += V^T P^T over NS x 32 keys
+template <int DH, int NS>
+__device__ __forceinline__ void pv_block(const VRead<DH>& v, int off, const f32x16 (&s)[NS], f32x16 (&o)[Tile<DH>::DT]) {
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+            bf16x8 pf;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pf[e] = f2bf(s[t][8 * k2 + e]);
+#pragma unroll
+            for (int dt = 0; dt < Tile<DH>::DT; ++dt)
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.frag(off, dt, t * 2 + k2), pf, o[dt], 0, 0, 0);
+        }
+}
+
+// the part of [first, last) (blocks) that split s of n takes
+__device__ __forceinline__ void split_blocks(int& first, int& last, int s, int n) {
+    const int c = (last - first + n - 1) / n;
+    first = min(first + s * c, last);
+    last = min(first + c, last);
+}
+
+// the lane's query row as right operand: dims 16 ks + 8 half .. + 7 (zeros from dh on)
+template <int KS>
+__device__ __forceinline__ void load_q(bf16x8 (&q)[KS], const bf16* p, int dh, int half) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int c = ks * 16 + half * 8;
+        bf16x8 z;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = f2bf(0.f);
+        q[ks] = c < dh ? *(const bf16x8*)(p + c) : z;
+    }
+}
+}  // namespace
+
+// --------------------------------------------------------------------------- bf16, many rows
+//
+// Four waves, 128 rows, blocks of 64 keys double-buffered in LDS (64 KB at 128 dims: two workgroups a
+// CU, whose softmax and matrix phases overlap).  The next block's loads are issued after the barrier that
+// opens a block and waited for at the next one.
+
+template <int DH, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a) {
+    using T = Tile<DH>;
+    constexpr int BKV = 64, NW = 4, NT = NW * 64, TB = BKV * T::P, LP = TB / (NT * 16), RP = NT / T::CH;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TB];  // K, V of buffer 0, then of buffer 1
+    __shared__ int wspan[NW][4];
+    __shared__ int odd_at[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const int G = a.H / a.Hk, nr = a.nq * G, nrb = gridDim.x / a.splits;
+    const int pos = tile_position((int)(blockIdx.y * gridDim.x + blockIdx.x), (int)(gridDim.x * gridDim.y));
+    const int bh = pos / (int)gridDim.x, rest = pos - bh * (int)gridDim.x, split = rest / nrb, rb = rest - split * nrb;
+    const int b = bh / a.Hk, hk = bh - b * a.Hk;
+    const int r = rb * (32 * NW) + wave * 32 + (lane & 31);
+    int i, h;
+    const Row w = row_info<CAP, BIAS>(a, b, hk, r, nr, G, i, h);
+    const Span ws = wave_span(w);
+    if (lane == 0) { wspan[wave][0] = ws.lo; wspan[wave][1] = ws.hi; wspan[wave][2] = ws.ilo; wspan[wave][3] = ws.ihi; }
+    if (tid < 2) odd_at[tid] = -1;
+    __syncthreads();
+    Span gs = ws;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+        gs.lo = min(gs.lo, wspan[k][0]);
+        gs.hi = max(gs.hi, wspan[k][1]);
+        gs.ilo = max(gs.ilo, wspan[k][2]);
+        gs.ihi = min(gs.ihi, wspan[k][3]);
+    }
+    gs.lo = __builtin_amdgcn_readfirstlane(gs.lo);
+    gs.hi = __builtin_amdgcn_readfirstlane(gs.hi);
+    gs.ilo = __builtin_amdgcn_readfirstlane(gs.ilo);
+    gs.ihi = __builtin_amdgcn_readfirstlane(gs.ihi);
+    int first = 0, last = 0;
+    if (gs.lo < gs.hi) {
+        first = gs.lo / BKV;
+        last = (gs.hi + BKV - 1) / BKV;
+    }
+    split_blocks(first, last, split, a.splits);
+
+    bf16x8 qf[T::KS];
+    load_q(qf, (const bf16*)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
+
+    const bf16* const K = (const bf16*)a.k + b * a.ks[0] + hk * a.ks[2];
+    const bf16* const V = (const bf16*)a.v + b * a.vs[0] + hk * a.vs[2];
+    // load part p: rows p RP + tid / CH, LDS chunk tid % CH
+    const int prow = tid / T::CH, pch = tid % T::CH;
+    unsigned ko[LP], vo[LP];
+#pragma unroll
+    for (int p = 0; p < LP; ++p) {
+        const int row = p * RP + prow, ck = T::kpos(row, pch), cv = T::vpos(row, pch);
+        ko[p] = ck * 8 < a.dh ? (unsigned)(row * a.ks[1] * 2 + ck * 16) : 0xFFFFFF00u;
+        vo[p] = cv * 8 < a.dh ? (unsigned)(row * a.vs[1] * 2 + cv * 16) : 0xFFFFFF00u;
+    }
+    const unsigned l0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
+    auto load = [&](int kb, int buf) {
+        const long k0 = (long)kb * BKV;
+        const unsigned rows = (unsigned)min((long)BKV, a.nk - k0) - 1;
+        const u32x4 rk = buf_desc(K + k0 * a.ks[1], rows * (unsigned)(a.ks[1] * 2) + a.dh * 2);
+        const u32x4 rv = buf_desc(V + k0 * a.vs[1], rows * (unsigned)(a.vs[1] * 2) + a.dh * 2);
+#pragma unroll
+        for (int p = 0; p < LP; ++p) dma16(l0 + buf * 2 * TB + p * NT * 16, ko[p], rk, 0);
+#pragma unroll
+        for (int p = 0; p < LP; ++p) dma16(l0 + buf * 2 * TB + TB + p * NT * 16, vo[p], rv, 0);
+    };
+    const char* kf[T::KS];
+#pragma unroll
+    for (int ks = 0; ks < T::KS; ++ks) kf[ks] = lds + (lane & 31) * T::P + T::kpos(lane & 31, ks * 2 + half) * 16;
+    const VRead<DH> vf(lds + TB, lane);
+
+    f32x16 o[T::DT];
+#pragma unroll
+    for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+    float m = -FLT_MAX, lsum = 0.f;
+    if (first < last) load(first, 0);
+    for (int kb = first; kb < last; ++kb) {
+        const int k0 = kb * BKV, buf = (kb - first) & 1, off = buf * 2 * TB;
+        const bool part = k0 < gs.ilo || k0 + BKV > gs.ihi;  // some row of the workgroup does not see all of it
+        vm_wait<0>();
+        if (part) {  // each thread looks over the values that it brought
+            bool odd = false;
+#pragma unroll
+            for (int p = 0; p < LP; ++p) odd |= clear_odd(lds + off + TB + p * NT * 16 + tid * 16);
+            if (odd) odd_at[buf] = kb;
+        }
+        __syncthreads();
+        if (kb + 1 < last) load(kb + 1, buf ^ 1);
+        if (k0 >= ws.hi || k0 + BKV <= ws.lo) continue;
+        f32x16 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < T::KS; ++ks)
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kf[ks] + off + t * 32 * T::P), qf[ks], s[t], 0, 0, 0);
+        }
+        const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
+        const float alpha = softmax_block<CAP, BIAS, 2>(s, w, k0 + half * 4, masked, m, lsum);
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f))
+#pragma unroll
+            for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+        pv_block<DH, 2>(vf, off, s, o);
+        if (part && __builtin_amdgcn_readfirstlane(odd_at[buf]) == kb)
+            add_odd<T::DT, bf16>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
+    }
+    finish<T::DT, bf16>(a, o, w, m, half_sum(lsum), split, b, hk, bh, r, nr, i, h, half);
+}
+
+// --------------------------------------------------------------------------- bf16, up to 32 rows
+//
+// The keys are read once, so the kernel is bound by memory: each of four waves takes every fourth
+// 32-key block of the workgroup's split, with two blocks of its own in LDS (32 KB a wave at 128 dims) and no
+// barrier until the waves' results are joined.
+
+template <int DH, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a) {
+    using T = Tile<DH>;
+    constexpr int BKV = 32, NW = 4, TB = BKV * T::P, LP = TB / 1024, RP = 64 / T::CH;
+    constexpr int MERGE = (T::DT * 16 + 2) * 64 * 4;
+    constexpr int BYTES = NW * 4 * TB > NW * MERGE ? NW * 4 * TB : NW * MERGE;
+    __shared__ __attribute__((aligned(1024))) char lds[BYTES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const int G = a.H / a.Hk, nr = a.nq * G;
+    const int pos = tile_position((int)(blockIdx.y * gridDim.x + blockIdx.x), (int)(gridDim.x * gridDim.y));
+    const int bh = pos / a.splits, split = pos - bh * a.splits;
+    const int b = bh / a.Hk, hk = bh - b * a.Hk;
+    const int r = lane & 31;
+    int i, h;
+    const Row w = row_info<CAP, BIAS>(a, b, hk, r, nr, G, i, h);
+    const Span ws = wave_span(w);
+    int first = 0, last = 0;
+    if (ws.lo < ws.hi) {
+        first = ws.lo / BKV;
+        last = (ws.hi + BKV - 1) / BKV;
+    }
+    split_blocks(first, last, split, a.splits);
+
+    bf16x8 qf[T::KS];
+    load_q(qf, (const bf16*)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
+    const bf16* const K = (const bf16*)a.k + b * a.ks[0] + hk * a.ks[2];
+    const bf16* const V = (const bf16*)a.v + b * a.vs[0] + hk * a.vs[2];
+    const int prow = lane / T::CH, pch = lane % T::CH;
+    unsigned ko[LP], vo[LP];
+#pragma unroll
+    for (int p = 0; p < LP; ++p) {
+        const int row = p * RP + prow, ck = T::kpos(row, pch), cv = T::vpos(row, pch);
+        ko[p] = ck * 8 < a.dh ? (unsigned)(row * a.ks[1] * 2 + ck * 16) : 0xFFFFFF00u;
+        vo[p] = cv * 8 < a.dh ? (unsigned)(row * a.vs[1] * 2 + cv * 16) : 0xFFFFFF00u;
+    }
+    char* const mine = lds + wave * 4 * TB;  // K, V of buffer 0, then of buffer 1
+    const unsigned l0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 4 * TB;
+    // block kb into a buffer; nothing but zeros past the last (the counted waits need every load)
+    auto load = [&](int kb, int buf) {
+        const bool in = kb < last;
+        const long k0 = in ? (long)kb * BKV : 0;
+        const unsigned rows = (unsigned)min((long)BKV, a.nk - k0) - 1;
+        const u32x4 rk = buf_desc(K + k0 * a.ks[1], in ? rows * (unsigned)(a.ks[1] * 2) + a.dh * 2 : 0);
+        const u32x4 rv = buf_desc(V + k0 * a.vs[1], in ? rows * (unsigned)(a.vs[1] * 2) + a.dh * 2 : 0);
+#pragma unroll
+        for (int p = 0; p < LP; ++p) dma16(l0 + buf * 2 * TB + p * 1024, ko[p], rk, 0);
+#pragma unroll
+        for (int p = 0; p < LP; ++p) dma16(l0 + buf * 2 * TB + TB + p * 1024, vo[p], rv, 0);
+    };
+    const char* kf[T::KS];
+#pragma unroll
+    for (int ks = 0; ks < T::KS; ++ks) kf[ks] = mine + (lane & 31) * T::P + T::kpos(lane & 31, ks * 2 + half) * 16;
+    const VRead<DH> vf(mine + TB, lane);
+    f32x16 o[T::DT];
+#pragma unroll
+    for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+    float m = -FLT_MAX, lsum = 0.f;
+    __builtin_amdgcn_s_waitcnt(0);  // the query rows are here: the counted waits below are about blocks only
+    load(first + wave, 0);
+    load(first + wave + NW, 1);
+    int buf = 0;
+    for (int kb = first + wave; kb < last; kb += NW, buf ^= 1) {
+        const int k0 = kb * BKV, off = buf * 2 * TB;
+        vm_wait<2 * LP>();
+        const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
+        bool odd = false;
+        if (masked) {
+#pragma unroll
+            for (int p = 0; p < LP; ++p) odd |= clear_odd(mine + off + TB + p * 1024 + lane * 16);
+        }
+        f32x16 s[1];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < T::KS; ++ks)
+            s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kf[ks] + off), qf[ks], s[0], 0, 0, 0);
+        const float alpha = softmax_block<CAP, BIAS, 1>(s, w, k0 + half * 4, masked, m, lsum);
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f))
+#pragma unroll
+            for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+        pv_block<DH, 1>(vf, off, s, o);
+        if (masked && __builtin_amdgcn_ballot_w64(odd))
+            add_odd<T::DT, bf16>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer has been read
+        load(kb + 2 * NW, buf);
+    }
+    vm_wait<0>();
+    __syncthreads();
+    // join the waves in their order
+    float* const mg = (float*)lds;
+    constexpr int ST = (T::DT * 16 + 2) * 64;
+    if (wave) {
+        float* const p = mg + wave * ST + lane;
+#pragma unroll
+        for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[(t * 16 + e) * 64] = o[t][e];
+        p[T::DT * 16 * 64] = m;
+        p[(T::DT * 16 + 1) * 64] = lsum;
+    }
+    __syncthreads();
+    if (wave) return;
+    float mx = m;
+#pragma unroll
+    for (int k = 1; k < NW; ++k) mx = fmaxf(mx, mg[k * ST + T::DT * 16 * 64 + lane]);
+    {
+        const float f = __builtin_amdgcn_exp2f(m - mx);
+        lsum *= f;
+#pragma unroll
+        for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] *= f;
+    }
+#pragma unroll
+    for (int k = 1; k < NW; ++k) {
+        const float* const p = mg + k * ST + lane;
+        const float f = __builtin_amdgcn_exp2f(p[T::DT * 16 * 64] - mx);
+        lsum = fmaf(p[(T::DT * 16 + 1) * 64], f, lsum);
+#pragma unroll
+        for (int t = 0; t < T::DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] = fmaf(p[(t * 16 + e) * 64], f, o[t][e]);
+    }
+    finish<T::DT, bf16>(a, o, w, mx, half_sum(lsum), split, b, hk, bh, r, nr, i, h, half);
+}
+
+// --------------------------------------------------------------------------- fp32
+//
+// The same with fp32 matrix instructions (32x32x2: a lane's left operand is one value): dims are taken in the
+// order 8 j + 4 half + 0..3, so that a lane reads four at once, and values as they lie in their
+// rows.  Blocks of 32 keys, staged through registers; four waves, 128 rows.
+
+template <int DH, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a) {
+    constexpr int BKV = 32, NW = 4, NT = 256, DT = DH / 32, J = DH / 8, P = DH + 4;  // padded rows
+    __shared__ __attribute__((aligned(16))) float sk[BKV * P], sv[BKV * P];
+    __shared__ int wspan[NW][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
+    const int G = a.H / a.Hk, nr = a.nq * G, nrb = gridDim.x / a.splits;
+    const int bh = blockIdx.y, split = blockIdx.x / nrb, rb = blockIdx.x - split * nrb;
+    const int b = bh / a.Hk, hk = bh - b * a.Hk;
+    const int r = rb * (32 * NW) + wave * 32 + l32;
+    int i, h;
+    const Row w = row_info<CAP, BIAS>(a, b, hk, r, nr, G, i, h);
+    const Span ws = wave_span(w);
+    if (lane == 0) { wspan[wave][0] = ws.lo; wspan[wave][1] = ws.hi; }
+    __syncthreads();
+    int lo = ws.lo, hi = ws.hi, first = 0, last = 0;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) { lo = min(lo, wspan[k][0]); hi = max(hi, wspan[k][1]); }
+    if (lo < hi) { first = lo / BKV; last = (hi + BKV - 1) / BKV; }
+    split_blocks(first, last, split, a.splits);
+    const float* const Q = (const float*)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
+    const float* const K = (const float*)a.k + b * a.ks[0] + hk * a.ks[2];
+    const float* const V = (const float*)a.v + b * a.vs[0] + hk * a.vs[2];
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x4 qf[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) qf[j] = 8 * j + 4 * half < a.dh ? *(const f32x4*)(Q + 8 * j + 4 * half) : zero;
+    f32x16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+    float m = -FLT_MAX, lsum = 0.f;
+    for (int kb = first; kb < last; ++kb) {
+        const int k0 = kb * BKV;
+        bool odd = false;
+        for (int x = tid; x < BKV * (DH / 4); x += NT) {
+            const int row = x / (DH / 4), c = (x - row * (DH / 4)) * 4;
+            const bool in = k0 + row < a.nk && c < a.dh;
+            const f32x4 kv = in ? *(const f32x4*)(K + (long)(k0 + row) * a.ks[1] + c) : zero;
+            f32x4 vv = in ? *(const f32x4*)(V + (long)(k0 + row) * a.vs[1] + c) : zero;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!(fabsf(vv[e]) <= FLT_MAX)) { odd = true; vv[e] = 0.f; }
+            *(f32x4*)(sk + row * P + c) = kv;
+            *(f32x4*)(sv + row * P + c) = vv;
+        }
+        odd = __builtin_amdgcn_readfirstlane(__syncthreads_or(odd));
+        if (k0 < ws.hi && k0 + BKV > ws.lo) {
+            f32x16 s[1];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const f32x4 kf = *(const f32x4*)(sk + l32 * P + 8 * j + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[j][e], s[0], 0, 0, 0);
+            }
+            const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
+            const float alpha = softmax_block<CAP, BIAS, 1>(s, w, k0 + half * 4, masked, m, lsum);
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+            const float* const vl = sv + half * 4 * P + l32;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vl[key_of(0, e) * P + t * 32], s[0][e], o[t], 0, 0, 0);
+            if (odd) add_odd<DT, float>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
+        }
+        __syncthreads();
+    }
+    finish<DT, float>(a, o, w, m, half_sum(lsum), split, b, hk, bh, r, nr, i, h, half);
+}
+
+// --------------------------------------------------------------------------- join of splits
+//
+// One thread per four dims of a row: O = sum_s O_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), splits in order.
+template <typename T>
+__global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
+    const int per = a.dh / 4;
+    const long G = a.H / a.Hk, nr = a.nq * G, n = (long)a.B * a.Hk * nr * per;
+    const long x = (long)blockIdx.x * 256 + threadIdx.x;
+    if (x >= n) return;
+    const int c = (int)(x % per) * 4;
+    const long row = x / per;  // over [bh][r]
+    const long bh = row / nr, r = row - bh * nr, stride = (long)a.B * a.Hk * nr * (a.dh + 4);
+    const float* const p = (const float*)a.work + row * (a.dh + 4);
+    float m = -FLT_MAX;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, p[s * stride + a.dh]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float* const ps = p + s * stride;
+        const float f = __builtin_amdgcn_exp2f(ps[a.dh] - m);
+        l = fmaf(ps[a.dh + 1], f, l);
+        o += *(const f32x4*)(ps + c) * f;
+    }
+    const bool some = !(p[a.dh + 1] < 0.f);
+    const float inv = 1.0f / l;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = some ? o[e] * inv : 0.f;
+    const long b = bh / a.Hk, hk = bh - b * a.Hk, i = r / G, h = hk * G + (r - i * G);
+    T* const dst = (T*)a.o + b * a.os[0] + i * a.os[1] + h * a.os[2] + c;
+    if constexpr (sizeof(T) == 2) store_bf16x4((bf16*)dst, v);
+    else *(f32x4*)dst = f32x4{v[0], v[1], v[2], v[3]};
+}
+
+// --------------------------------------------------------------------------- dispatch
+
+static bool few_rows(int bf, const RangeAttnArgs& a) { return bf && (long)a.nq * (a.H / a.Hk) <= 32; }
+
+// Splits that give every CU work, and at least 256 keys each (few rows: 128 to a wave)
+int range_attention_splits(int bf, const RangeAttnArgs& a) {
+    const long nr = (long)a.nq * (a.H / a.Hk), groups = (long)a.B * a.Hk * ((nr + 127) / 128);
+    const long want = few_rows(bf, a) ? 512 : 256;
+    const long most = few_rows(bf, a) ? a.nk / 512 : a.nk / 256;
+    return (int)std::max(1L, std::min({want / groups, most, 64L}));
+}
+
+size_t range_attention_bytes(const RangeAttnArgs& a, int splits) {
+    return splits <= 1 ? 0 : (size_t)splits * a.B * a.H * a.nq * (a.dh + 4) * sizeof(float);
+}
+
+template <int DH, bool CAP, bool BIAS>
+static void range_run(int bf, const RangeAttnArgs& a, hipStream_t st) {
+    const long nr = (long)a.nq * (a.H / a.Hk);
+    const dim3 grid((unsigned)((nr + 127) / 128 * a.splits), (unsigned)(a.B * a.Hk));
+    if (!bf) range_attn_f32_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
+    else if (few_rows(bf, a)) range_attn_few_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
+    else range_attn_bf16_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
+}
+template <int DH>
+static void range_modes(int bf, const RangeAttnArgs& a, hipStream_t st) {
+    if (a.cap > 0.f) a.slopes ? range_run<DH, true, true>(bf, a, st) : range_run<DH, true, false>(bf, a, st);
+    else a.slopes ? range_run<DH, false, true>(bf, a, st) : range_run<DH, false, false>(bf, a, st);
+}
+
+hipError_t launch_range_attention(int bf, const RangeAttnArgs& a, hipStream_t st) {
+    if (a.dh <= 64) range_modes<64>(bf, a, st);
+    else if (a.dh <= 96) range_modes<96>(bf, a, st);
+    else range_modes<128>(bf, a, st);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits <= 1) return e;
+    const long n = (long)a.B * a.H * a.nq * (a.dh / 4);
+    const dim3 grid((unsigned)((n + 255) / 256));
+    if (bf) range_attn_join_kernel<bf16><<<grid, 256, 0, st>>>(a);
+    else range_attn_join_kernel<float><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace sgd

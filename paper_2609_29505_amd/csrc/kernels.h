@@ -155,6 +155,60 @@ hipError_t launch_sumsq(const float* x, const float* y, float* copy, int B, int 
                         int have_y, double* partial, hipStream_t st);
 hipError_t launch_sumsq_finish(const double* partial, int count, double* out, hipStream_t st);
 
+// ---------------------------------------------------------------- microscaled rows (mx.h)
+constexpr int MX_FP8 = 0, MX_FP4 = 1;  // e4m3, e2m1 elements
+struct MxQuantArgs {
+    const void* x = nullptr;  // source rows (quantisation), ldx elements apart
+    void* out = nullptr;      // read back: where to, ldx apart
+    long ldx = 0;
+    int rows = 0, K = 0;
+    uint8_t* codes = nullptr; uint8_t* scales = nullptr;
+};
+// bf: x / out is bf16 (0: fp32).  rows * K / 8 < 2^31
+hipError_t launch_mx_quantize(int fmt, int bf, const MxQuantArgs& a, hipStream_t st);
+hipError_t launch_mx_dequantize(int fmt, int bf, const MxQuantArgs& a, hipStream_t st);
+// h = x + r (r may be null: h = x, nothing is written to xo), xo = h in x's type, codes and scales of
+// h / sqrt(mean(h^2) + eps) * w; rows of d <= 8192 values, d % 32 == 0
+struct NormMxArgs {
+    const void* x; const void* r; void* xo; const float* w; float eps; int M, d;
+    uint8_t* codes; uint8_t* scales;
+};
+hipError_t launch_norm_add_mx(int fmt, int x_bf, int r_bf, const NormMxArgs& a, hipStream_t st);
+// C = A W^T with A in format fmt and W in e2m1 (both K columns, compact rows), by a kernel of
+// gemm_mx.hip: tile 0 automatic, 1..6 block tiles (256x256, 256x128, 128x256, 128x128, 128x64, 64x64),
+// kMxTiles the kernel for up to 16 rows.  Epilogues EP_ACT, EP_GATED (g.N = 2 F) and EP_PARTIAL
+// (ksplit 1: fp32 rows e.d apart, to e.h).
+constexpr int kMxTiles = 7;
+struct MxScales { const uint8_t* a; const uint8_t* w; };
+bool gemm_mx_shape_ok(int fmt, const GemmArgs& g, const EpiParams& e, int tile);
+hipError_t launch_gemm_mx(int fmt, const GemmArgs& g, const EpiParams& e, const MxScales& s, int tile, hipStream_t st);
+
+// ---------------------------------------------------------------- rotary positions
+// T tokens of H heads, last dim contiguous; token and head strides in elements.  turns: fp64 [rot / 2].
+struct RotaryArgs {
+    const void* x; void* out; long x_ts, x_hs, o_ts, o_hs;
+    const double* turns; const int32_t* pos;  // pos null: token t is at position t
+    int T, H, dh, rot, interleaved, inverse; float magnitude;
+};
+hipError_t launch_rotary(int bf, const RotaryArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- attention over key intervals
+// Query i of sample b sees the keys [max(0, lo), min(nk, hi)) of ranges[b][i] = {lo, hi}.  Rows of q, k, v, o:
+// last dim contiguous, strides (batch, token, head) in elements.  H = Hk x G query heads, G to a key head.
+struct RangeAttnArgs {
+    const void* q; const void* k; const void* v; void* o;
+    long qs[3], ks[3], vs[3], os[3];
+    const int32_t* ranges; const int32_t* pos;  // pos null: query i is at key position i + nk - nq
+    const float* slopes;                        // [H] or null
+    int B, H, Hk, dh, nq, nk;
+    float scale, cap;                           // cap 0: none
+    void* work; int splits;
+};
+// key ranges per row block that the launch uses, and the workspace they need (0 bytes: none)
+int range_attention_splits(int bf, const RangeAttnArgs& a);
+size_t range_attention_bytes(const RangeAttnArgs& a, int splits);
+hipError_t launch_range_attention(int bf, const RangeAttnArgs& a, hipStream_t st);
+
 // ---------------------------------------------------------------- spectra (fp64)
 // One scored matrix of a batch: X rows x cols; its Gram matrix is X^T X (trans = 0, n = cols) or
 // X X^T (trans = 1, n = rows); k is the spectral rank of its score; tile0 is the first of its tiles in the
