@@ -6,6 +6,7 @@ Every computation runs in ``libsgd.so``.  Torch tensors supply device buffers
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -92,8 +93,8 @@ class sgd_rope_params(C.Structure):
 
 class sgd_range_attention(C.Structure):
     _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("o", C.c_void_p),
-                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
-                ("o_stride", C.c_int64 * 3), ("ranges", C.c_void_p), ("pos", C.c_void_p), ("slopes", C.c_void_p),
+                ("strides", C.c_int64 * 12),  # q_stride, k_stride, v_stride, o_stride
+                ("ranges", C.c_void_p), ("pos", C.c_void_p), ("slopes", C.c_void_p),
                 ("B", C.c_int32), ("H", C.c_int32), ("Hk", C.c_int32), ("dh", C.c_int32), ("nq", C.c_int32),
                 ("nk", C.c_int32), ("scale", C.c_float), ("cap", C.c_float)]
 
@@ -466,32 +467,48 @@ def op_frozen_run(h, deltas, stream=None) -> None:
     _check(lib().sgd_op_frozen_run(_p(h), arr, len(deltas), h.numel(), C.c_void_p(_stream_ptr(stream))))
 
 
-def _expect(t, name, dtype, shape, contiguous=True) -> None:
-    """The tensors of a call agree with each other (the library sees pointers only)."""
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or (contiguous and not t.is_contiguous()):
-        raise ValueError(f"{name}: expected a {'contiguous ' if contiguous else ''}device tensor {dtype} {tuple(shape)}, "
-                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+# The operators below check that the tensors of a call agree with each other, since the library sees pointers only.
+# A call costs the host a few microseconds, which is what a single token's kernels take: addresses go as
+# plain integers, the current device is asked for once and the stream's handle without a Stream object.
 
-
-def _one_device(*tensors) -> None:
+def _here(stream):
+    """(current device, stream handle) of a call."""
     import torch
-    for t in tensors:
-        if t is not None and t.device.index != torch.cuda.current_device():
-            raise ValueError(f"a tensor on {t.device}, the current device is {torch.cuda.current_device()}")
+    dev = torch._C._cuda_getDevice()
+    return dev, (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+
+
+def _at(t, dev, name, dtype, shape, contiguous=True) -> int:
+    """The address of tensor ``t`` after checking its device, type and shape."""
+    if t.get_device() != dev or t.dtype != dtype or t.shape != shape or (contiguous and not t.is_contiguous()):
+        raise ValueError(f"{name}: expected a {'contiguous ' if contiguous else ''}tensor {dtype} {tuple(shape)} on the current "
+                         f"device {dev}, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _row_stride(t, name, rows, K) -> int:
+    """Row stride of a 2-D tensor [rows, K] whose rows are contiguous."""
+    if K > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous, got strides {t.stride()}")
+    return t.stride(0) if rows > 1 else K
 
 
 class MxTensor:
     """Microscaled rows (see sgd_ops.h): ``fmt`` "fp8" or "fp4", ``codes`` uint8 [rows, K or K / 2], ``scales`` uint8
     [ceil(K / 256), rows, 8]."""
 
+    __slots__ = ("fmt", "format", "codes", "scales", "rows", "K")
+
     def __init__(self, fmt: str, codes, scales):
         import torch
-        self.fmt, self.codes, self.scales = fmt, codes, scales
+        self.fmt, self.format, self.codes, self.scales = fmt, SGD_MX[fmt], codes, scales
         if codes.dim() != 2:
             raise ValueError("codes are [rows, bytes of a row]")
-        self.rows, self.K = codes.shape[0], codes.shape[1] * (1 if SGD_MX[fmt] == 0 else 2)
-        _expect(codes, "codes", torch.uint8, codes.shape)
-        _expect(scales, "scales", torch.uint8, (-(-self.K // 256), self.rows, 8))
+        self.rows, row = codes.shape
+        self.K = row if fmt == "fp8" else 2 * row
+        dev = codes.get_device()
+        _at(codes, dev, "codes", torch.uint8, codes.shape)
+        _at(scales, dev, "scales", torch.uint8, (-(-self.K // 256), self.rows, 8))
 
     @classmethod
     def empty(cls, fmt: str, rows: int, K: int) -> "MxTensor":
@@ -501,61 +518,63 @@ class MxTensor:
         return cls(fmt, torch.empty(rows, nc.value // rows, dtype=torch.uint8, device="cuda"),
                    torch.empty(-(-K // 256), rows, 8, dtype=torch.uint8, device="cuda"))
 
-
-def _rows2d(t, name, rows, K) -> int:
-    """Row stride of a 2-D device tensor with contiguous rows."""
-    if not t.is_cuda or tuple(t.shape) != (rows, K) or (K > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: expected a device tensor {(rows, K)} with contiguous rows, got {tuple(t.shape)}")
-    return t.stride(0) if rows > 1 else K
+    def at(self, dev):
+        """Addresses of codes and scales."""
+        if self.codes.get_device() != dev or self.scales.get_device() != dev:
+            raise ValueError(f"microscaled rows on {self.codes.device}, the current device is {dev}")
+        return self.codes.data_ptr(), self.scales.data_ptr()
 
 
 def op_mx_quantize(x, mx: MxTensor, stream=None) -> None:
     """x [rows, K] (bf16 or fp32, rows strided) into ``mx``."""
-    _one_device(x, mx.codes, mx.scales)
-    ld = _rows2d(x, "x", mx.rows, mx.K)
-    _check(lib().sgd_op_mx_quantize(SGD_MX[mx.fmt], _dtype_code(x), _p(x), ld, mx.rows, mx.K, _p(mx.codes),
-                                    _p(mx.scales), C.c_void_p(_stream_ptr(stream))))
+    dev, st = _here(stream)
+    px = _at(x, dev, "x", x.dtype, (mx.rows, mx.K), False)
+    pc, ps = mx.at(dev)
+    _check(lib().sgd_op_mx_quantize(mx.format, _dtype_code(x), px, _row_stride(x, "x", mx.rows, mx.K), mx.rows, mx.K, pc,
+                                    ps, st))
 
 
 def op_mx_dequantize(mx: MxTensor, out, stream=None) -> None:
     """The values of ``mx`` into out [rows, K] (bf16 or fp32, rows strided)."""
-    _one_device(out, mx.codes, mx.scales)
-    ld = _rows2d(out, "out", mx.rows, mx.K)
-    _check(lib().sgd_op_mx_dequantize(SGD_MX[mx.fmt], _p(mx.codes), _p(mx.scales), mx.rows, mx.K, _dtype_code(out),
-                                      _p(out), ld, C.c_void_p(_stream_ptr(stream))))
+    dev, st = _here(stream)
+    po = _at(out, dev, "out", out.dtype, (mx.rows, mx.K), False)
+    pc, ps = mx.at(dev)
+    _check(lib().sgd_op_mx_dequantize(mx.format, pc, ps, mx.rows, mx.K, _dtype_code(out), po,
+                                      _row_stride(out, "out", mx.rows, mx.K), st))
 
 
 def op_linear_mx(A: MxTensor, W: MxTensor, out, bias=None, act=0, gated=False, tile=0, stream=None) -> None:
     """out [M, N] = act(A W^T + bias); gated: W = [W_gate; W_up] with 2 N rows.  W in "fp4"."""
     import torch
-    _one_device(A.codes, A.scales, W.codes, W.scales, out, bias)
+    dev, st = _here(stream)
     n = W.rows // 2 if gated else W.rows
     if W.fmt != "fp4" or W.K != A.K or (gated and W.rows % 2):
         raise ValueError(f"W must be fp4 rows of A's {A.K} columns (gated: an even number of them)")
-    ldo = _rows2d(out, "out", A.rows, n)
-    if bias is not None:
-        _expect(bias, "bias", torch.float32, (W.rows,))
-    _check(lib().sgd_op_linear_mx(SGD_MX[A.fmt], _p(A.codes), _p(A.scales), _p(W.codes), _p(W.scales), _p(bias),
-                                  _dtype_code(out), _p(out), ldo, A.rows, n, A.K, act, int(gated), tile,
-                                  C.c_void_p(_stream_ptr(stream))))
+    pa, sa = A.at(dev)
+    pw, sw = W.at(dev)
+    po = _at(out, dev, "out", out.dtype, (A.rows, n), False)
+    pb = None if bias is None else _at(bias, dev, "bias", torch.float32, (W.rows,))
+    _check(lib().sgd_op_linear_mx(A.format, pa, sa, pw, sw, pb, _dtype_code(out), po, _row_stride(out, "out", A.rows, n),
+                                  A.rows, n, A.K, act, int(gated), tile, st))
 
 
 def op_norm_add_mx(x, w, mx: MxTensor, eps, add=None, out=None, stream=None) -> None:
     """h = x + add, out = h (None: written back to x), mx = h / rms(h) * w; without ``add`` h = x and nothing but
     ``mx`` is written."""
     import torch
-    xo = None if add is None else x if out is None else out
-    _one_device(x, w, mx.codes, mx.scales, add, xo)
-    _expect(x, "x", x.dtype, (mx.rows, mx.K))
-    _expect(w, "w", torch.float32, (mx.K,))
+    dev, st = _here(stream)
+    shape = (mx.rows, mx.K)
+    px = _at(x, dev, "x", x.dtype, shape)
+    pw = _at(w, dev, "w", torch.float32, (mx.K,))
+    pa = po = None
     if add is not None:
-        _expect(add, "add", add.dtype, (mx.rows, mx.K))
-        _expect(xo, "out", x.dtype, (mx.rows, mx.K))
+        pa = _at(add, dev, "add", add.dtype, shape)
+        po = px if out is None else _at(out, dev, "out", x.dtype, shape)
     elif out is not None:
         raise ValueError("without add there is no sum to write to out")
-    _check(lib().sgd_op_norm_add_mx(SGD_MX[mx.fmt], _dtype_code(x), _p(x), 0 if add is None else _dtype_code(add), _p(add),
-                                    _p(xo), _p(w), eps, mx.rows, mx.K, _p(mx.codes), _p(mx.scales),
-                                    C.c_void_p(_stream_ptr(stream))))
+    pc, ps = mx.at(dev)
+    _check(lib().sgd_op_norm_add_mx(mx.format, _dtype_code(x), px, 0 if add is None else _dtype_code(add), pa, po, pw, eps,
+                                    mx.rows, mx.K, pc, ps, st))
 
 
 def rope_turns(rot, base=10000.0, scaling="plain", factor=1.0, context=0.0, low=1.0, high=32.0):
@@ -571,17 +590,30 @@ def op_rotary(x, out, turns, pos=None, interleaved=False, magnitude=1.0, inverse
     """Rotates the first 2 len(turns) dims of x [T, H, dh] by ``pos`` (int32 [T]; None: the token's index) into
     ``out`` (may be x); ``turns``: float64 device tensor, as from rope_turns."""
     import torch
-    _one_device(x, out, turns, pos)
-    if x.dim() != 3 or x.stride(2) != 1 or out.stride(-1) != 1:
-        raise ValueError("x and out are [T, H, dh] with contiguous heads")
+    dev, st = _here(stream)
+    if x.dim() != 3:
+        raise ValueError("x is [T, H, dh]")
     T, H, dh = x.shape
-    _expect(out, "out", x.dtype, x.shape, contiguous=False)
-    _expect(turns, "turns", torch.float64, (turns.numel(),))
-    if pos is not None:
-        _expect(pos, "pos", torch.int32, (T,))
-    _check(lib().sgd_op_rotary(_dtype_code(x), _p(x), x.stride(0), x.stride(1), _p(out), out.stride(0), out.stride(1),
-                               T, H, dh, 2 * turns.numel(), int(interleaved), _p(pos), _p(turns), magnitude,
-                               int(inverse), C.c_void_p(_stream_ptr(stream))))
+    px = _at(x, dev, "x", x.dtype, (T, H, dh), False)
+    po = _at(out, dev, "out", x.dtype, (T, H, dh), False)
+    xt, xh, xd = x.stride()
+    ot, oh, od = out.stride()
+    if dh > 1 and (xd != 1 or od != 1):
+        raise ValueError("heads must be contiguous")
+    n = turns.numel()
+    pt = _at(turns, dev, "turns", torch.float64, (n,))
+    pp = None if pos is None else _at(pos, dev, "pos", torch.int32, (T,))
+    _check(lib().sgd_op_rotary(_dtype_code(x), px, xt, xh, po, ot, oh, T, H, dh, 2 * n, int(interleaved), pp, pt, magnitude,
+                               int(inverse), st))
+
+
+@functools.lru_cache(maxsize=4096)
+def _range_bytes(dt, B, H, Hk, dh, nq, nk) -> int:
+    """Workspace of a shape; what else a call needs is checked when it is made."""
+    c = sgd_range_attention(None, None, None, None, (C.c_int64 * 12)(*[1 << 12] * 12), None, None, None, B, H, Hk, dh, nq, nk, 0.0, 0.0)
+    nb = C.c_size_t()
+    _check(lib().sgd_op_attention_ranges_bytes(dt, C.byref(c), C.byref(nb)))
+    return nb.value
 
 
 def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, pos=None, workspace=None, stream=None) -> None:
@@ -589,33 +621,34 @@ def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, po
     strides free), query (b, i) seeing the keys ranges[b, i] = (lo, hi) (int32 [B, nq, 2]); see sgd_ops.h.
     ``workspace``: a uint8 device tensor for the calls that need one (None: allocated here)."""
     import torch
-    _one_device(q, k, v, o, ranges, slopes, pos, workspace)
+    dev, st = _here(stream)
     B, nq, H, dh = q.shape
-    nk, Hk = k.shape[1], k.shape[2]
-    _expect(k, "k", q.dtype, (B, nk, Hk, dh), contiguous=False)
-    _expect(v, "v", q.dtype, (B, nk, Hk, dh), contiguous=False)
-    _expect(o, "o", q.dtype, (B, nq, H, dh), contiguous=False)
-    _expect(ranges, "ranges", torch.int32, (B, nq, 2))
-    if any(t.stride(3) != 1 for t in (q, k, v, o)):
+    _, nk, Hk, _ = k.shape
+    kv = (B, nk, Hk, dh)
+    pq, pk = _at(q, dev, "q", q.dtype, (B, nq, H, dh), False), _at(k, dev, "k", q.dtype, kv, False)
+    pv, po = _at(v, dev, "v", q.dtype, kv, False), _at(o, dev, "o", q.dtype, (B, nq, H, dh), False)
+    pr = _at(ranges, dev, "ranges", torch.int32, (B, nq, 2))
+    psl = None if slopes is None else _at(slopes, dev, "slopes", torch.float32, (H,))
+    pp = None if pos is None else _at(pos, dev, "pos", torch.int32, (B, nq))
+    q0, q1, q2, q3 = q.stride()
+    k0, k1, k2, k3 = k.stride()
+    v0, v1, v2, v3 = v.stride()
+    o0, o1, o2, o3 = o.stride()
+    if not q3 == k3 == v3 == o3 == 1:
         raise ValueError("heads must be contiguous")
-    if slopes is not None:
-        _expect(slopes, "slopes", torch.float32, (H,))
-    if pos is not None:
-        _expect(pos, "pos", torch.int32, (B, nq))
-    st = [(C.c_int64 * 3)(*t.stride()[:3]) for t in (q, k, v, o)]
-    c = sgd_range_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), *st, ranges.data_ptr(),
-                            pos.data_ptr() if pos is not None else None,
-                            slopes.data_ptr() if slopes is not None else None, B, H, Hk, dh, nq, nk,
-                            0.0 if scale is None else scale, cap)
     dt = _dtype_code(q)
-    nb = C.c_size_t()
-    _check(lib().sgd_op_attention_ranges_bytes(dt, C.byref(c), C.byref(nb)))
-    sp = C.c_void_p(_stream_ptr(stream))
-    if nb.value and workspace is None:
-        workspace = _workspace(nb.value)
+    c = sgd_range_attention(pq, pk, pv, po, (q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2), pr, pp, psl, B, H, Hk, dh, nq, nk,
+                            0.0 if scale is None else scale, cap)
+    need = _range_bytes(dt, B, H, Hk, dh, nq, nk)
+    pws = nws = 0
+    if need and workspace is None:
+        workspace = _workspace(need)
         if stream is not None:
             workspace.record_stream(stream)  # it may be freed here while the call is still to run there
-    _check(lib().sgd_op_attention_ranges(dt, C.byref(c), _p(workspace), workspace.numel() if workspace is not None else 0, sp))
+    if workspace is not None:
+        nws = workspace.numel()
+        pws = _at(workspace, dev, "workspace", torch.uint8, (nws,))
+    _check(lib().sgd_op_attention_ranges(dt, C.byref(c), pws, nws, st))
 
 
 # ------------------------------------------------------------------ model

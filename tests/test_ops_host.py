@@ -88,9 +88,8 @@ def _call(**kw):
     d = dict(q=A, k=B, v=D, o=E, q_stride=(512, 256, 64), k_stride=(512, 256, 64), v_stride=(512, 256, 64), o_stride=(512, 256, 64), ranges=F,
              pos=None, slopes=None, B=1, H=4, Hk=4, dh=64, nq=2, nk=2, scale=0.0, cap=0.0)
     d.update(kw)
-    st = lambda t: (C.c_int64 * 3)(*t)  # noqa: E731
-    return sgd_range_attention(d["q"], d["k"], d["v"], d["o"], st(d["q_stride"]), st(d["k_stride"]), st(d["v_stride"]), st(d["o_stride"]),
-                               d["ranges"], d["pos"], d["slopes"], d["B"], d["H"], d["Hk"], d["dh"], d["nq"], d["nk"], d["scale"], d["cap"])
+    strides = (*d["q_stride"], *d["k_stride"], *d["v_stride"], *d["o_stride"])
+    return sgd_range_attention(d["q"], d["k"], d["v"], d["o"], strides, d["ranges"], d["pos"], d["slopes"], d["B"], d["H"], d["Hk"], d["dh"], d["nq"], d["nk"], d["scale"], d["cap"])
 
 
 @pytest.mark.parametrize("dt,change,code", [
