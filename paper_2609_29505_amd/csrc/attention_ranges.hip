@@ -49,17 +49,54 @@ struct Row {
     float c0, c1;    // scores: raw c0 (no cap), or c0 (1 - 2 / (1 + 2^(raw c1)))
 };
 
-// Row r of key head hk (nr rows), sample b; rows past the last see nothing
+// The work of a workgroup: a row block and a split of a key head's rows.  Each XCD takes an eighth of the heads
+// (tile_order.h), all of them at once, and row blocks from the last to the first: under a causal mask or a prefix
+// the long ones start first (8192 causal tokens, 16 heads: 341 us head by head and forwards, 302 so).
+struct Place { int bh, b, hk, split, rb, G, nr; };
+__device__ __forceinline__ Place place_of(const RangeAttnArgs& a, int bx) {
+    Place p;
+    p.G = a.H / a.Hk;
+    p.nr = a.nq * p.G;
+    const int per = gridDim.x, heads = gridDim.y, nrb = per / a.splits;
+    const int at_once = heads % kXcds ? 1 : heads / kXcds;
+    const int pos = tile_position(bx, per * heads);
+    const int grp = pos / (at_once * per), rest = pos - grp * (at_once * per), rev = rest / at_once;
+    p.bh = grp * at_once + (rest - rev * at_once);
+    p.split = (per - 1 - rev) / nrb;
+    p.rb = per - 1 - rev - p.split * nrb;
+    p.b = p.bh / a.Hk;
+    p.hk = p.bh - p.b * a.Hk;
+    return p;
+}
+__device__ __forceinline__ int block_number() { return (int)(blockIdx.y * gridDim.x + blockIdx.x); }
+// The kernel's arguments read again, and its block number computed again, through values that the compiler
+// cannot see through: the end of a kernel holds no scalars over its main loop
+__device__ __forceinline__ const RangeAttnArgs& args_again() {
+    const char __attribute__((address_space(4)))* args =
+        (const char __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    return *(const RangeAttnArgs*)(const char*)args;
+}
+__device__ __forceinline__ int block_again() {
+    int n = block_number();
+    asm volatile("" : "+s"(n));
+    return n;
+}
+
+// Query and head of row r of a place's key head (rows past the last: the last one's)
+__device__ __forceinline__ void row_place(const Place& p, int r, int& i, int& h) {
+    const int rc = min(r, p.nr - 1);
+    i = rc / p.G;
+    h = p.hk * p.G + (rc - i * p.G);
+}
+// What its lane knows of it; rows past the last see nothing
 template <bool CAP, bool BIAS>
-__device__ __forceinline__ Row row_info(const RangeAttnArgs& a, int b, int hk, int r, int nr, int G, int& i, int& h) {
-    const int rc = min(r, nr - 1);
-    i = rc / G;
-    h = hk * G + (rc - i * G);
+__device__ __forceinline__ Row row_info(const RangeAttnArgs& a, const Place& p, int r, int i, int h) {
     Row w;
-    const long at = (long)b * a.nq + i;
+    const long at = (long)p.b * a.nq + i;
     w.lo = max(a.ranges[2 * at], 0);
     w.hi = min(a.ranges[2 * at + 1], a.nk);
-    if (r >= nr || w.lo >= w.hi) w.lo = w.hi = 0;
+    if (r >= p.nr || w.lo >= w.hi) w.lo = w.hi = 0;
     w.pos = BIAS ? (a.pos ? a.pos[at] : i + a.nk - a.nq) : 0;
     w.slope = BIAS ? a.slopes[h] * kLog2e : 0.f;
     w.c0 = (CAP ? a.cap : a.scale) * kLog2e;
@@ -94,16 +131,24 @@ __device__ __forceinline__ constexpr int key_of(int t, int r) { return t * 32 + 
 // the lane's partial sum go on; returns the factor for what was accumulated before.
 template <bool CAP, bool BIAS, int NS>
 __device__ __forceinline__ float softmax_block(f32x16 (&s)[NS], const Row& w, int key0, bool masked, float& m, float& lsum) {
-    constexpr bool LATE = !CAP && !BIAS;  // the plain scale is folded into the exponent
-    if constexpr (!LATE) {
+    // Without a bias a score's last step, x -> x sf + sb, is folded into the exponent: s holds the raw score (sf = c0,
+    // sb = 0) or, capped, R = 1 / (1 + 2^(raw c1)) (sf = -2 c0, sb = c0), and what is masked the value of score -inf
+    constexpr bool LATE = !BIAS;
+    const float sf = LATE ? (CAP ? -2.0f * w.c0 : w.c0) : 1.0f, sb = LATE && CAP ? w.c0 : 0.f;
+    const float none = LATE && CAP ? INFINITY : -INFINITY;
+    if constexpr (CAP || BIAS) {
         const float d0 = BIAS ? (float)(w.pos - key0) : 0.f;
 #pragma unroll
         for (int t = 0; t < NS; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 float x = s[t][r];
-                if constexpr (CAP) x = w.c0 - 2.0f * w.c0 * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * w.c1));
-                else x *= w.c0;
+                if constexpr (CAP) {
+                    x = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * w.c1));
+                    if constexpr (BIAS) x = fmaf(-2.0f * w.c0, x, w.c0);
+                } else {
+                    x *= w.c0;
+                }
                 if constexpr (BIAS) x = fmaf(-w.slope, fabsf(d0 - (float)key_of(t, r)), x);
                 s[t][r] = x;
             }
@@ -113,16 +158,19 @@ __device__ __forceinline__ float softmax_block(f32x16 (&s)[NS], const Row& w, in
 #pragma unroll
         for (int t = 0; t < NS; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if ((unsigned)key_of(t, r) - a >= n) s[t][r] = -INFINITY;
+            for (int r = 0; r < 16; ++r) {
+                if ((unsigned)key_of(t, r) - a >= n) s[t][r] = none;
+                if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // a few conditions at a time: they take scalars
+            }
     }
+    constexpr float sign = LATE && CAP ? -1.0f : 1.0f;  // the largest score has the smallest R
     float bm = -INFINITY;
 #pragma unroll
     for (int t = 0; t < NS; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, s[t][r]);
+        for (int r = 0; r < 16; ++r) bm = fmaxf(bm, sign * s[t][r]);
     bm = half_max(bm);
-    if constexpr (LATE) bm *= w.c0;
+    if constexpr (LATE) bm = fmaf(sign * bm, sf, sb);
     float alpha = 1.0f;
     if (__builtin_amdgcn_ballot_w64(bm > m + kSlack)) {
         const float mn = fmaxf(m, bm);
@@ -130,12 +178,13 @@ __device__ __forceinline__ float softmax_block(f32x16 (&s)[NS], const Row& w, in
         m = mn;
         lsum *= alpha;
     }
+    const float at = sb - m;
     float ps = 0.f;
 #pragma unroll
     for (int t = 0; t < NS; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const float p = __builtin_amdgcn_exp2f(LATE ? fmaf(s[t][r], w.c0, -m) : s[t][r] - m);
+            const float p = __builtin_amdgcn_exp2f(LATE ? fmaf(s[t][r], sf, at) : s[t][r] - m);
             s[t][r] = p;
             ps += p;
         }
@@ -150,41 +199,63 @@ __device__ __forceinline__ float* partial_row(const RangeAttnArgs& a, int split,
 }
 
 // A lane's O^T (dims dt 32 + 8 (r / 4) + 4 half + r % 4 of its row), maximum and whole sum: divided and
-// stored, or left for the join
+// stored, or left for the join.  A wave's bf16 rows go through LDS (stage: 32 rows of DT 64 + 16 bytes of the wave's
+// own): straight from the registers a store would touch 16 bytes of each of 32 rows.
 template <int DT, typename T>
-__device__ __forceinline__ void finish(const RangeAttnArgs& a, const f32x16 (&o)[DT], const Row& w, float m, float l, int split,
-                                       int b, int hk, int bh, int r, int nr, int i, int h, int half) {
-    if (r >= nr) return;
+__device__ __forceinline__ void finish(const f32x16 (&o)[DT], const Row& w, float m, float l, int wave_row, int lane, char* stage) {
+    const RangeAttnArgs& a = args_again();
+    const Place pl = place_of(a, block_again());
+    const int half = lane >> 5, r0 = pl.rb * 128 + wave_row, r = r0 + (lane & 31);
     const bool some = w.lo < w.hi;
-    if (a.splits > 1) {
-        float* const p = partial_row(a, split, bh, r);
+    const float inv = 1.0f / l;
+    int dh = a.dh;
+    if (a.splits > 1 || sizeof(T) == 4) {
+        if (r >= pl.nr) return;
+        int i, h;
+        row_place(pl, r, i, h);
+        float* const dst = a.splits > 1 ? partial_row(a, pl.split, pl.bh, r) : (float*)a.o + pl.b * a.os[0] + i * a.os[1] + h * a.os[2];
+        const float f = a.splits > 1 ? 1.f : some ? inv : 0.f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int d = dt * 32 + g * 8 + half * 4;
-                if (d < a.dh) *(f32x4*)(p + d) = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+                asm volatile("" : "+s"(dh));  // one condition at a time
+                if (dt * 32 + g * 8 >= dh) continue;
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = a.splits > 1 || some ? o[dt][4 * g + e] * f : 0.f;
+                *(f32x4*)(dst + dt * 32 + g * 8 + half * 4) = v;
             }
-        if (half == 0) {
-            p[a.dh] = m;
-            p[a.dh + 1] = some ? l : -1.0f;  // -1: the row sees nothing
+        if (a.splits > 1 && half == 0) {
+            dst[dh] = m;
+            dst[dh + 1] = some ? l : -1.0f;  // -1: the row sees nothing
         }
         return;
     }
-    T* const dst = (T*)a.o + b * a.os[0] + i * a.os[1] + h * a.os[2];
-    const float inv = 1.0f / l;
+    if constexpr (sizeof(T) == 2) {
+        constexpr int P = DT * 64 + 16;  // bytes of a staged row
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int d = dt * 32 + g * 8 + half * 4;
-            if (d >= a.dh) continue;
-            float v[4];
+            for (int g = 0; g < 4; ++g) {
+                float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = some ? o[dt][4 * g + e] * inv : 0.f;
-            if constexpr (sizeof(T) == 2) store_bf16x4((bf16*)dst + d, v);
-            else *(f32x4*)(dst + d) = f32x4{v[0], v[1], v[2], v[3]};
+                for (int e = 0; e < 4; ++e) v[e] = some ? o[dt][4 * g + e] * inv : 0.f;
+                store_bf16x4((bf16*)(stage + (lane & 31) * P) + dt * 32 + g * 8 + half * 4, v);
+            }
+        asm volatile("" ::: "memory");  // the reads stay behind the writes (a wave's LDS operations are in order)
+        const int per = dh / 8;  // 16-byte pieces of a row
+        for (int x = lane; x < 32 * per; x += 64) {
+            const int row = x / per, c = x - row * per;
+            if (r0 + row >= pl.nr) break;
+            int i, h;
+            row_place(pl, r0 + row, i, h);
+            const u32x4 v = *(const u32x4*)(stage + row * P + c * 16);
+            bf16* const dst = (bf16*)a.o + pl.b * a.os[0] + i * a.os[1] + h * a.os[2] + c * 8;
+            *(u32x2*)dst = u32x2{v[0], v[1]};
+            *(u32x2*)(dst + 4) = u32x2{v[2], v[3]};
         }
+    }
 }
 
 // Bits of a pair of bf16 values: 0x8000 in each half that holds an infinity or a NaN
@@ -303,8 +374,8 @@ __device__ __forceinline__ void load_q(bf16x8 (&q)[KS], const bf16* p, int dh, i
 // --------------------------------------------------------------------------- bf16, many rows
 //
 // Four waves, 128 rows, blocks of 64 keys double-buffered in LDS (64 KB at 128 dims: two workgroups a
-// CU, whose softmax and matrix phases overlap).  The next block's loads are issued after the barrier that
-// opens a block and waited for at the next one.
+// CU, one's vector instructions under the other's matrix instructions).  The next block's loads are issued after the
+// barrier that opens a block and waited for at the next one.
 
 template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a) {
@@ -314,13 +385,13 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
     __shared__ int wspan[NW][4];
     __shared__ int odd_at[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-    const int G = a.H / a.Hk, nr = a.nq * G, nrb = gridDim.x / a.splits;
-    const int pos = tile_position((int)(blockIdx.y * gridDim.x + blockIdx.x), (int)(gridDim.x * gridDim.y));
-    const int bh = pos / (int)gridDim.x, rest = pos - bh * (int)gridDim.x, split = rest / nrb, rb = rest - split * nrb;
-    const int b = bh / a.Hk, hk = bh - b * a.Hk;
-    const int r = rb * (32 * NW) + wave * 32 + (lane & 31);
+    const Place pl = place_of(a, block_number());
+    const int r = pl.rb * 128 + wave * 32 + (lane & 31);
     int i, h;
-    const Row w = row_info<CAP, BIAS>(a, b, hk, r, nr, G, i, h);
+    row_place(pl, r, i, h);
+    bf16x8 qf[T::KS];
+    load_q(qf, (const bf16*)a.q + pl.b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
+    const Row w = row_info<CAP, BIAS>(a, pl, r, i, h);
     const Span ws = wave_span(w);
     if (lane == 0) { wspan[wave][0] = ws.lo; wspan[wave][1] = ws.hi; wspan[wave][2] = ws.ilo; wspan[wave][3] = ws.ihi; }
     if (tid < 2) odd_at[tid] = -1;
@@ -342,13 +413,10 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
         first = gs.lo / BKV;
         last = (gs.hi + BKV - 1) / BKV;
     }
-    split_blocks(first, last, split, a.splits);
+    split_blocks(first, last, pl.split, a.splits);
 
-    bf16x8 qf[T::KS];
-    load_q(qf, (const bf16*)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
-
-    const bf16* const K = (const bf16*)a.k + b * a.ks[0] + hk * a.ks[2];
-    const bf16* const V = (const bf16*)a.v + b * a.vs[0] + hk * a.vs[2];
+    const bf16* const K = (const bf16*)a.k + pl.b * a.ks[0] + pl.hk * a.ks[2];
+    const bf16* const V = (const bf16*)a.v + pl.b * a.vs[0] + pl.hk * a.vs[2];
     // load part p: rows p RP + tid / CH, LDS chunk tid % CH
     const int prow = tid / T::CH, pch = tid % T::CH;
     unsigned ko[LP], vo[LP];
@@ -360,6 +428,7 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
     }
     const unsigned l0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
     auto load = [&](int kb, int buf) {
+        asm volatile("" : "+s"(kb));  // the addresses are computed here, not carried through the loop
         const long k0 = (long)kb * BKV;
         const unsigned rows = (unsigned)min((long)BKV, a.nk - k0) - 1;
         const u32x4 rk = buf_desc(K + k0 * a.ks[1], rows * (unsigned)(a.ks[1] * 2) + a.dh * 2);
@@ -381,6 +450,9 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
         for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
     float m = -FLT_MAX, lsum = 0.f;
     if (first < last) load(first, 0);
+    // the query rows are here: left open, the compiler would wait for them, and with them for the next
+    // block's loads, before the first matrix instruction of every block
+    __builtin_amdgcn_s_waitcnt(0);
     for (int kb = first; kb < last; ++kb) {
         const int k0 = kb * BKV, buf = (kb - first) & 1, off = buf * 2 * TB;
         const bool part = k0 < gs.ilo || k0 + BKV > gs.ihi;  // some row of the workgroup does not see all of it
@@ -395,13 +467,34 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
         if (kb + 1 < last) load(kb + 1, buf ^ 1);
         if (k0 >= ws.hi || k0 + BKV <= ws.lo) continue;
         f32x16 s[2];
+        // Wide heads: all of K's fragments are read first, then half of V's between the scores' instructions (4096
+        // tokens, 32 heads of 128 dims: 266 us, left to the compiler 272; of 64 dims 176 and 162)
+        constexpr bool AHEAD = DH > 64;
+        constexpr int NK = 2 * T::KS, NV = 4 * T::DT, NP = AHEAD ? NV / 2 : 0;
+        bf16x8 kr[AHEAD ? NK : 1], vr[AHEAD ? NP : 1];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+        if constexpr (AHEAD) {
 #pragma unroll
-            for (int ks = 0; ks < T::KS; ++ks)
-                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kf[ks] + off + t * 32 * T::P), qf[ks], s[t], 0, 0, 0);
+            for (int x = 0; x < NK; ++x) kr[x] = *(const bf16x8*)(kf[x >> 1] + off + (x & 1) * 32 * T::P);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int x = 0; x < NK; ++x) {
+                s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[x], qf[x >> 1], s[x & 1], 0, 0, 0);
+#pragma unroll
+                for (int y = x * NP / NK; y < (x + 1) * NP / NK; ++y) vr[y] = vf.frag(off, y % T::DT, y / T::DT);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int ks = 0; ks < T::KS; ++ks)
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kf[ks] + off + t * 32 * T::P), qf[ks], s[t], 0, 0, 0);
         }
         const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
         const float alpha = softmax_block<CAP, BIAS, 2>(s, w, k0 + half * 4, masked, m, lsum);
@@ -410,11 +503,22 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
             for (int t = 0; t < T::DT; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
-        pv_block<DH, 2>(vf, off, s, o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            bf16x8 pf;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pf[e] = f2bf(s[k >> 1][8 * (k & 1) + e]);
+#pragma unroll
+            for (int dt = 0; dt < T::DT; ++dt) {
+                const int y = k * T::DT + dt;
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y < NP ? vr[y < NP ? y : 0] : vf.frag(off, dt, k), pf, o[dt], 0, 0, 0);
+            }
+        }
         if (part && __builtin_amdgcn_readfirstlane(odd_at[buf]) == kb)
             add_odd<T::DT, bf16>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
     }
-    finish<T::DT, bf16>(a, o, w, m, half_sum(lsum), split, b, hk, bh, r, nr, i, h, half);
+    __syncthreads();  // the blocks' LDS is free
+    finish<T::DT, bf16>(o, w, m, half_sum(lsum), wave * 32, lane, lds + wave * 32 * (T::DT * 64 + 16));
 }
 
 // --------------------------------------------------------------------------- bf16, up to 32 rows
@@ -431,25 +535,22 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
     constexpr int BYTES = NW * 4 * TB > NW * MERGE ? NW * 4 * TB : NW * MERGE;
     __shared__ __attribute__((aligned(1024))) char lds[BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-    const int G = a.H / a.Hk, nr = a.nq * G;
-    const int pos = tile_position((int)(blockIdx.y * gridDim.x + blockIdx.x), (int)(gridDim.x * gridDim.y));
-    const int bh = pos / a.splits, split = pos - bh * a.splits;
-    const int b = bh / a.Hk, hk = bh - b * a.Hk;
-    const int r = lane & 31;
+    const Place pl = place_of(a, block_number());
     int i, h;
-    const Row w = row_info<CAP, BIAS>(a, b, hk, r, nr, G, i, h);
+    row_place(pl, lane & 31, i, h);
+    bf16x8 qf[T::KS];
+    load_q(qf, (const bf16*)a.q + pl.b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
+    const Row w = row_info<CAP, BIAS>(a, pl, lane & 31, i, h);
     const Span ws = wave_span(w);
     int first = 0, last = 0;
     if (ws.lo < ws.hi) {
         first = ws.lo / BKV;
         last = (ws.hi + BKV - 1) / BKV;
     }
-    split_blocks(first, last, split, a.splits);
+    split_blocks(first, last, pl.split, a.splits);
 
-    bf16x8 qf[T::KS];
-    load_q(qf, (const bf16*)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
-    const bf16* const K = (const bf16*)a.k + b * a.ks[0] + hk * a.ks[2];
-    const bf16* const V = (const bf16*)a.v + b * a.vs[0] + hk * a.vs[2];
+    const bf16* const K = (const bf16*)a.k + pl.b * a.ks[0] + pl.hk * a.ks[2];
+    const bf16* const V = (const bf16*)a.v + pl.b * a.vs[0] + pl.hk * a.vs[2];
     const int prow = lane / T::CH, pch = lane % T::CH;
     unsigned ko[LP], vo[LP];
 #pragma unroll
@@ -482,7 +583,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
     float m = -FLT_MAX, lsum = 0.f;
-    __builtin_amdgcn_s_waitcnt(0);  // the query rows are here: the counted waits below are about blocks only
+    __builtin_amdgcn_s_waitcnt(0);  // the query rows are here (as above; not after the two loads, whose wait is counted)
     load(first + wave, 0);
     load(first + wave + NW, 1);
     int buf = 0;
@@ -550,7 +651,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[t][e] = fmaf(p[(t * 16 + e) * 64], f, o[t][e]);
     }
-    finish<T::DT, bf16>(a, o, w, mx, half_sum(lsum), split, b, hk, bh, r, nr, i, h, half);
+    finish<T::DT, bf16>(o, w, mx, half_sum(lsum), 0, lane, lds);
 }
 
 // --------------------------------------------------------------------------- fp32
@@ -565,12 +666,10 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
     __shared__ __attribute__((aligned(16))) float sk[BKV * P], sv[BKV * P];
     __shared__ int wspan[NW][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
-    const int G = a.H / a.Hk, nr = a.nq * G, nrb = gridDim.x / a.splits;
-    const int bh = blockIdx.y, split = blockIdx.x / nrb, rb = blockIdx.x - split * nrb;
-    const int b = bh / a.Hk, hk = bh - b * a.Hk;
-    const int r = rb * (32 * NW) + wave * 32 + l32;
+    const Place pl = place_of(a, block_number());
     int i, h;
-    const Row w = row_info<CAP, BIAS>(a, b, hk, r, nr, G, i, h);
+    row_place(pl, pl.rb * 128 + wave * 32 + l32, i, h);
+    const Row w = row_info<CAP, BIAS>(a, pl, pl.rb * 128 + wave * 32 + l32, i, h);
     const Span ws = wave_span(w);
     if (lane == 0) { wspan[wave][0] = ws.lo; wspan[wave][1] = ws.hi; }
     __syncthreads();
@@ -578,10 +677,10 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
 #pragma unroll
     for (int k = 0; k < NW; ++k) { lo = min(lo, wspan[k][0]); hi = max(hi, wspan[k][1]); }
     if (lo < hi) { first = lo / BKV; last = (hi + BKV - 1) / BKV; }
-    split_blocks(first, last, split, a.splits);
-    const float* const Q = (const float*)a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
-    const float* const K = (const float*)a.k + b * a.ks[0] + hk * a.ks[2];
-    const float* const V = (const float*)a.v + b * a.vs[0] + hk * a.vs[2];
+    split_blocks(first, last, pl.split, a.splits);
+    const float* const Q = (const float*)a.q + pl.b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
+    const float* const K = (const float*)a.k + pl.b * a.ks[0] + pl.hk * a.ks[2];
+    const float* const V = (const float*)a.v + pl.b * a.vs[0] + pl.hk * a.vs[2];
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     f32x4 qf[J];
 #pragma unroll
@@ -633,37 +732,41 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
         }
         __syncthreads();
     }
-    finish<DT, float>(a, o, w, m, half_sum(lsum), split, b, hk, bh, r, nr, i, h, half);
+    finish<DT, float>(o, w, m, half_sum(lsum), wave * 32, lane, nullptr);
 }
 
 // --------------------------------------------------------------------------- join of splits
 //
-// One thread per four dims of a row: O = sum_s O_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), splits in order.
+// A workgroup per row: O = sum_s O_s 2^(m_s - m) / sum_s l_s 2^(m_s - m).  Lane s of every wave holds split s's maximum
+// and factor; lane % 32 takes four dims, and the eight half waves every eighth split each (64 splits of 16 rows:
+// one wave a row 12.4 us).
 template <typename T>
 __global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
-    const int per = a.dh / 4;
-    const long G = a.H / a.Hk, nr = a.nq * G, n = (long)a.B * a.Hk * nr * per;
-    const long x = (long)blockIdx.x * 256 + threadIdx.x;
-    if (x >= n) return;
-    const int c = (int)(x % per) * 4;
-    const long row = x / per;  // over [bh][r]
-    const long bh = row / nr, r = row - bh * nr, stride = (long)a.B * a.Hk * nr * (a.dh + 4);
+    __shared__ f32x4 part[8][32];
+    const int lane = threadIdx.x & 63, eighth = threadIdx.x >> 5, c = (lane & 31) * 4;
+    const long G = a.H / a.Hk, nr = a.nq * G, row = blockIdx.x;  // over [bh][r]
+    const long stride = (long)a.B * a.Hk * nr * (a.dh + 4);
     const float* const p = (const float*)a.work + row * (a.dh + 4);
-    float m = -FLT_MAX;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, p[s * stride + a.dh]);
+    const float m = lane < a.splits ? p[lane * stride + a.dh] : -FLT_MAX;
+    const float l = lane < a.splits ? p[lane * stride + a.dh + 1] : 0.f;
+    const bool some = !__builtin_amdgcn_ballot_w64(l < 0.f);
+    const float f = __builtin_amdgcn_exp2f(m - warp_max(m));
+    const float inv = 1.0f / warp_sum(l * f);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float* const ps = p + s * stride;
-        const float f = __builtin_amdgcn_exp2f(ps[a.dh] - m);
-        l = fmaf(ps[a.dh + 1], f, l);
-        o += *(const f32x4*)(ps + c) * f;
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {
+        const int s = s0 + eighth;
+        const float fs = __shfl(f, s & 63, 64);
+        if (s < a.splits && c < a.dh) o += *(const f32x4*)(p + s * stride + c) * fs;
     }
-    const bool some = !(p[a.dh + 1] < 0.f);
-    const float inv = 1.0f / l;
+    part[eighth][lane & 31] = o;
+    __syncthreads();
+    if (threadIdx.x >= 32 || c >= a.dh) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) o += part[k][lane];
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = some ? o[e] * inv : 0.f;
+    const long bh = row / nr, r = row - bh * nr;
     const long b = bh / a.Hk, hk = bh - b * a.Hk, i = r / G, h = hk * G + (r - i * G);
     T* const dst = (T*)a.o + b * a.os[0] + i * a.os[1] + h * a.os[2] + c;
     if constexpr (sizeof(T) == 2) store_bf16x4((bf16*)dst, v);
@@ -674,12 +777,11 @@ __global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
 
 static bool few_rows(int bf, const RangeAttnArgs& a) { return bf && (long)a.nq * (a.H / a.Hk) <= 32; }
 
-// Splits that give every CU work, and at least 256 keys each (few rows: 128 to a wave)
+// Splits that give every CU one workgroup and each of them at least 256 keys (the kernel for few rows has one
+// workgroup a CU: 16384 keys, 32 key heads, 8 splits 70 us, 16 in two rounds 77, 32 92)
 int range_attention_splits(int bf, const RangeAttnArgs& a) {
     const long nr = (long)a.nq * (a.H / a.Hk), groups = (long)a.B * a.Hk * ((nr + 127) / 128);
-    const long want = few_rows(bf, a) ? 512 : 256;
-    const long most = few_rows(bf, a) ? a.nk / 512 : a.nk / 256;
-    return (int)std::max(1L, std::min({want / groups, most, 64L}));
+    return (int)std::max(1L, std::min({256L / groups, a.nk / 256L, 64L}));
 }
 
 size_t range_attention_bytes(const RangeAttnArgs& a, int splits) {
@@ -706,8 +808,7 @@ hipError_t launch_range_attention(int bf, const RangeAttnArgs& a, hipStream_t st
     else range_modes<128>(bf, a, st);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits <= 1) return e;
-    const long n = (long)a.B * a.H * a.nq * (a.dh / 4);
-    const dim3 grid((unsigned)((n + 255) / 256));
+    const dim3 grid((unsigned)((long)a.B * a.H * a.nq));
     if (bf) range_attn_join_kernel<bf16><<<grid, 256, 0, st>>>(a);
     else range_attn_join_kernel<float><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
