@@ -147,8 +147,8 @@ int sgd_op_mx_dequantize(int32_t format, const void* codes, const uint8_t* scale
  * [2N x K] = [W_gate; W_up]) in SGD_MX_FP4.  out_dtype SGD_BF16, or SGD_F32 (ungated, act SGD_ACT_NONE); rows of
  * out ldo elements apart.  Products are exact and summed in fp32; with A in e4m3 the matrix cores align 64
  * products to their largest and drop what lies about 16 bits below it (up to 5e-5 of the result's size
- * where A's codes span the format's whole range).  tile: 0 auto, 1..6 block tiles (256x256, 256x128, 128x256,
- * 128x128, 128x64, 64x64), 7 the kernel for up to 16 rows.  N % 4 == 0 (gated: N % 32 == 0, and on a fixed
+ * where A's codes span the format's whole range).  tile: 0 auto, 1..7 block tiles (256x256, 256x192, 256x128,
+ * 128x256, 128x128, 128x64, 64x64), 8 the kernel for up to 16 rows.  N % 4 == 0 (gated: N % 32 == 0, and on a fixed
  * tile 2N a multiple of its width), bias 16-byte, out 8-byte (fp32: 16-byte) aligned, ldo % 4 == 0, each
  * operand's scales and W's codes below 4 GiB. */
 int sgd_op_linear_mx(int32_t a_format, const void* a_codes, const uint8_t* a_scales, const void* w_codes,

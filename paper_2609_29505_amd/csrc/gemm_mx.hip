@@ -101,12 +101,12 @@ struct MxPPCfg {
     static constexpr int RW = BH / WGM;                  // a wave's rows of each half
     static constexpr int CB = RW / 32, TM = 2 * CB;      // MFMA row blocks per half, per wave
     static constexpr int WN = BN / WGN, TN = WN / 32;
-    static constexpr int BP = BN / K::BROWS, BL = BP / 2;  // W parts per tile; those loaded in phase 1
-    static constexpr int A_HALF = BH * 128, A_STAGE = BM * 128, B_STAGE = BN * K::WB;
+    static constexpr int BP = (BN + K::BROWS - 1) / K::BROWS, BL = BP / 2;  // W parts per tile; those loaded in phase 1
+    static constexpr int A_HALF = BH * 128, A_STAGE = BM * 128, B_STAGE = BP * 8192;
     static constexpr int SC = ((BM + BN) * K::SB + 2047) / 2048, S_STAGE = SC * 2048;  // scales: A's rows, then W's
     static constexpr int B_LDS = ST * A_STAGE, S_LDS = B_LDS + ST * B_STAGE, LDS_BYTES = S_LDS + ST * S_STAGE;
     __device__ static __forceinline__ int block_row(int wm, int i) { return (i / CB) * BH + wm * RW + (i % CB) * 32; }
-    static_assert(WGM * WGN == NW && RW % 32 == 0 && WN % 32 == 0 && BN % K::BROWS == 0 && BH % 64 == 0, "wave tile");
+    static_assert(WGM * WGN == NW && RW % 32 == 0 && WN % 32 == 0 && BH % 64 == 0, "wave tile");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS");
 };
 
@@ -184,12 +184,17 @@ __global__ __launch_bounds__(C::NT, 2) void gemm_mx_pp_kernel(GemmArgs g, EpiPar
     constexpr int WC = K::WB / 16;
     const int wrow = wave * (64 / WC) + lane / WC, wchunk = K::wpos(wrow, lane % WC);
     const int ra = FA == MX_FP8 ? g.K : g.K / 2, rw = g.K / 2;
-    // part 0; the others follow at even distances (a W part covers whole waves' columns).  Rows past M or N are
-    // past the buffer's range
+    // Part 0; A's others follow at even distances, and W's do where a part is whole waves' columns.  Rows past M or N
+    // are past the buffer's range
+    constexpr bool EVEN = K::BROWS % C::WN == 0;
     const unsigned aoff = (unsigned)(arow * ra + achunk * 16);
-    const unsigned boff = (unsigned)(weight_row<C>(ep, g.N / 2, tn, wrow) * rw + wchunk * 16);
-    static_assert(K::BROWS % C::WN == 0 && C::WN % 64 == 0, "W parts");
     const int astep = 64 * ra, bstep = (int)(weight_row<C>(ep, g.N / 2, tn, K::BROWS) - weight_row<C>(ep, g.N / 2, tn, 0)) * rw;
+    unsigned boff[EVEN ? 1 : C::BP];
+#pragma unroll
+    for (int p = 0; p < (EVEN ? 1 : C::BP); ++p) {
+        const int r = p * K::BROWS + wrow;
+        boff[p] = r < C::BN ? (unsigned)(weight_row<C>(ep, g.N / 2, tn, r) * rw + wchunk * 16) : kMxOob;
+    }
     unsigned soff[C::SC];
 #pragma unroll
     for (int p = 0; p < C::SC; ++p) soff[p] = mx_scale_off<C>(g, ep, m0, tn, p * 512 + tid);
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(C::NT, 2) void gemm_mx_pp_kernel(GemmArgs g, EpiPar
         asm volatile("" : "+s"(step));
 #pragma unroll
         for (int p = decltype(from)::value; p < decltype(to)::value; ++p)
-            dma16(lw + C::B_LDS + stage * C::B_STAGE + p * 8192, last ? kMxOob : boff + p * step, r, in ? t * K::WB : 0);
+            dma16(lw + C::B_LDS + stage * C::B_STAGE + p * 8192, last ? kMxOob : EVEN ? boff[0] + p * step : boff[EVEN ? 0 : p], r, in ? t * K::WB : 0);
     };
     auto load_s = [&](int t, int stage) {
         const bool in = t < KT;
@@ -656,6 +661,7 @@ namespace {
 template <int FA> using X256x256 = MxPPCfg<FA, 256, 256, 2, 4>;
 template <int FA> using X256x128 = MxPPCfg<FA, 256, 128, 4, 2, 3>;
 template <int FA> using X128x256 = MxPPCfg<FA, 128, 256, 2, 4, 3>;
+template <int FA> using X256x192 = MxPPCfg<FA, 256, 192, 4, 2>;
 template <int FA> using X128x128 = MxPKCfg<FA, 128, 128, 2>;
 template <int FA> using X128x64 = MxPKCfg<FA, 128, 64, 3>;
 template <int FA> using X64x64 = MxPKCfg<FA, 64, 64, 4>;
@@ -665,11 +671,12 @@ struct Shape { int bm, bn; double t0, t1, fix; };
 Shape tile_shape(int tile) {
     switch (tile) {
         case 1: return {256, 256, 0.8, 1.5, 7.5};
-        case 2: return {256, 128, 0.6, 0.9, 3.0};
-        case 3: return {128, 256, 0.7, 1.0, 2.5};
-        case 4: return {128, 128, 0.32, 0.6, 2.1};
-        case 5: return {128, 64, 0.30, 0.41, 1.9};
-        case 6: return {64, 64, 0.15, 0.26, 2.4};
+        case 2: return {256, 192, 0.7, 1.25, 5.5};
+        case 3: return {256, 128, 0.6, 0.9, 3.0};
+        case 4: return {128, 256, 0.7, 1.0, 2.5};
+        case 5: return {128, 128, 0.32, 0.6, 2.1};
+        case 6: return {128, 64, 0.30, 0.41, 1.9};
+        case 7: return {64, 64, 0.15, 0.26, 2.4};
         default: return {0, 0, 0.0, 0.0, 0.0};
     }
 }
@@ -686,7 +693,7 @@ static double tile_cost(int tile, int fmt, const GemmArgs& g, const EpiParams& e
 
 int gemm_mx_tile(int fmt, const GemmArgs& g, const EpiParams& e) {
     if (g.M <= 16) return kMxTiles;
-    int best = 6;
+    int best = 7;
     double best_t = 1e300;
     for (int tile = 1; tile < kMxTiles; ++tile) {
         const double t = tile_cost(tile, fmt, g, e);
@@ -727,11 +734,12 @@ template <int FA>
 static hipError_t run_mx_tile(const GemmArgs& g, const EpiParams& e, const MxScales& s, int tile, hipStream_t st) {
     switch (tile) {
         case 1: return run_mx<X256x256<FA>>(g, e, s, st);
-        case 2: return run_mx<X256x128<FA>>(g, e, s, st);
-        case 3: return run_mx<X128x256<FA>>(g, e, s, st);
-        case 4: return run_mx<X128x128<FA>>(g, e, s, st);
-        case 5: return run_mx<X128x64<FA>>(g, e, s, st);
-        case 6: return run_mx<X64x64<FA>>(g, e, s, st);
+        case 2: return run_mx<X256x192<FA>>(g, e, s, st);
+        case 3: return run_mx<X256x128<FA>>(g, e, s, st);
+        case 4: return run_mx<X128x256<FA>>(g, e, s, st);
+        case 5: return run_mx<X128x128<FA>>(g, e, s, st);
+        case 6: return run_mx<X128x64<FA>>(g, e, s, st);
+        case 7: return run_mx<X64x64<FA>>(g, e, s, st);
         default: break;
     }
     const int nout = e.kind == EP_GATED ? e.F : g.N;

@@ -175,10 +175,10 @@ struct NormMxArgs {
 };
 hipError_t launch_norm_add_mx(int fmt, int x_bf, int r_bf, const NormMxArgs& a, hipStream_t st);
 // C = A W^T with A in format fmt and W in e2m1 (both K columns, compact rows), by a kernel of
-// gemm_mx.hip: tile 0 automatic, 1..6 block tiles (256x256, 256x128, 128x256, 128x128, 128x64, 64x64),
-// kMxTiles the kernel for up to 16 rows.  Epilogues EP_ACT, EP_GATED (g.N = 2 F) and EP_PARTIAL
+// gemm_mx.hip: tile 0 automatic, 1..7 block tiles (256x256, 256x192, 256x128, 128x256, 128x128, 128x64,
+// 64x64), kMxTiles the kernel for up to 16 rows.  Epilogues EP_ACT, EP_GATED (g.N = 2 F) and EP_PARTIAL
 // (ksplit 1: fp32 rows e.d apart, to e.h).
-constexpr int kMxTiles = 7;
+constexpr int kMxTiles = 8;
 struct MxScales { const uint8_t* a; const uint8_t* w; };
 bool gemm_mx_shape_ok(int fmt, const GemmArgs& g, const EpiParams& e, int tile);
 hipError_t launch_gemm_mx(int fmt, const GemmArgs& g, const EpiParams& e, const MxScales& s, int tile, hipStream_t st);

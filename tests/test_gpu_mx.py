@@ -157,11 +157,11 @@ LINEAR = [(1, 64, 64), (1, 580, 4096), (16, 260, 160), (17, 64, 96), (33, 132, 2
 
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
 @pytest.mark.parametrize("M,N,K", LINEAR)
-@pytest.mark.parametrize("tile", [0, 1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("tile", [0, 1, 2, 3, 4, 5, 6, 7, 8])
 def test_linear(P, fmt, M, N, K, tile):
     """Every tile, both outputs, with and without bias; rows and columns past the output stay as they were."""
     import torch
-    if tile == 7 and M > 16:
+    if tile == 8 and M > 16:
         pytest.skip("the kernel for up to 16 rows")
     rng, A, a, W, w = linear_case(P, fmt, M, N, K, M + N + K)
     b = 0.1 * rng.standard_normal(N)
@@ -178,8 +178,8 @@ def test_linear(P, fmt, M, N, K, tile):
 
 
 @pytest.mark.parametrize("fmt", ["fp8", "fp4"])
-@pytest.mark.parametrize("M,N,K,tile", [(1, 64, 256, 0), (16, 96, 4096, 7), (5, 32, 96, 6), (130, 256, 288, 1), (130, 256, 288, 2), (260, 384, 160, 3),
-                                        (200, 128, 512, 4), (70, 160, 224, 5), (70, 160, 224, 6), (300, 1152, 320, 0)])
+@pytest.mark.parametrize("M,N,K,tile", [(1, 64, 256, 0), (16, 96, 4096, 8), (5, 32, 96, 7), (130, 256, 288, 1), (130, 288, 288, 2), (130, 256, 288, 3),
+                                        (260, 384, 160, 4), (200, 128, 512, 5), (70, 160, 224, 6), (70, 160, 224, 7), (300, 1152, 320, 0)])
 @pytest.mark.parametrize("act", [0, 1, 2, 3])
 def test_linear_act_and_gate(P, fmt, M, N, K, tile, act):
     import torch
@@ -215,7 +215,7 @@ def test_linear_whole_range(P, fmt):
     sa[0, 3, 2] = 255  # a NaN block spoils its row, and no other
     a, w = R.decode(ca, sa, fmt), R.decode(cw, sw, "fp4")
     A, W = (P.MxTensor(f, torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda()) for f, c, s in ((fmt, ca, sa), ("fp4", cw, sw)))
-    for tile in (0, 1, 4, 6):
+    for tile in (0, 1, 2, 5, 7):
         out = torch.empty(M, N, device="cuda")
         P.op_linear_mx(A, W, out, tile=tile)
         got = host(out)

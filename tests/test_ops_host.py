@@ -51,10 +51,10 @@ def test_quantize_refuses(L, change, code):
 
 @pytest.mark.parametrize("change,code", [
     (dict(a=None), ARG), (dict(sw=None), ARG), (dict(out=None), ARG), (dict(fmt=3), DTYPE), (dict(odt=2), DTYPE), (dict(act=4), ARG),
-    (dict(tile=8), ARG), (dict(tile=-1), ARG), (dict(odt=0, act=1), DTYPE), (dict(odt=0, gated=1), DTYPE), (dict(M=0), SHAPE), (dict(N=6), SHAPE),
+    (dict(tile=9), ARG), (dict(tile=-1), ARG), (dict(odt=0, act=1), DTYPE), (dict(odt=0, gated=1), DTYPE), (dict(M=0), SHAPE), (dict(N=6), SHAPE),
     (dict(K=16), SHAPE), (dict(K=80), SHAPE), (dict(gated=1, N=36, ldo=36), SHAPE), (dict(ldo=60), ARG), (dict(ldo=66), ARG), (dict(out=E + 4), ARG),
     (dict(odt=0, out=E + 8), ARG), (dict(bias=F + 4), ARG), (dict(a=A + 8), ARG), (dict(w=B + 8), ARG), (dict(sa=D + 4), ARG),
-    (dict(tile=7, M=17), SHAPE), (dict(tile=1, gated=1, N=64), SHAPE), (dict(N=1 << 22, ldo=1 << 22, K=1 << 12), SHAPE)])
+    (dict(tile=8, M=17), SHAPE), (dict(tile=1, gated=1, N=64), SHAPE), (dict(N=1 << 22, ldo=1 << 22, K=1 << 12), SHAPE)])
 def test_linear_refuses(L, change, code):
     a = dict(fmt=0, a=A, sa=D, w=B, sw=D, bias=None, odt=1, out=E, ldo=64, M=4, N=64, K=64, act=0, gated=0, tile=0)
     a.update(change)
