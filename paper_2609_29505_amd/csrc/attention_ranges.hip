@@ -129,11 +129,14 @@ __device__ __forceinline__ constexpr int key_of(int t, int r) { return t * 32 + 
 // One block's softmax: raw scores s (key of register (t, r): key0 + key_of(t, r)) become probabilities.  The
 // running maximum m (log2 domain; -FLT_MAX before the first visible key, so that no difference is NaN) and
 // the lane's partial sum go on; returns the factor for what was accumulated before.
-template <bool CAP, bool BIAS, int NS>
+// EXACT (fp32 tensors): the cap by tanhf, right to fp32 rounding of small scores too.  Otherwise cap tanh(x / cap) =
+// cap - 2 cap R, which is off by 2^-24 cap whatever the score: 2e-6 of a probability at cap 30, where bf16
+// probabilities are off by 2e-3.
+template <bool CAP, bool BIAS, bool EXACT, int NS>
 __device__ __forceinline__ float softmax_block(f32x16 (&s)[NS], const Row& w, int key0, bool masked, float& m, float& lsum) {
     // Without a bias a score's last step, x -> x sf + sb, is folded into the exponent: s holds the raw score (sf = c0,
     // sb = 0) or, capped, R = 1 / (1 + 2^(raw c1)) (sf = -2 c0, sb = c0), and what is masked the value of score -inf
-    constexpr bool LATE = !BIAS;
+    constexpr bool LATE = !BIAS && !(CAP && EXACT);
     const float sf = LATE ? (CAP ? -2.0f * w.c0 : w.c0) : 1.0f, sb = LATE && CAP ? w.c0 : 0.f;
     const float none = LATE && CAP ? INFINITY : -INFINITY;
     if constexpr (CAP || BIAS) {
@@ -143,7 +146,9 @@ __device__ __forceinline__ float softmax_block(f32x16 (&s)[NS], const Row& w, in
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 float x = s[t][r];
-                if constexpr (CAP) {
+                if constexpr (CAP && EXACT) {
+                    x = w.c0 * tanhf(x * (w.c1 * 0.5f / kLog2e));
+                } else if constexpr (CAP) {
                     x = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * w.c1));
                     if constexpr (BIAS) x = fmaf(-2.0f * w.c0, x, w.c0);
                 } else {
@@ -401,13 +406,12 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
     for (int k = 0; k < NW; ++k) {
         gs.lo = min(gs.lo, wspan[k][0]);
         gs.hi = max(gs.hi, wspan[k][1]);
-        gs.ilo = max(gs.ilo, wspan[k][2]);
-        gs.ihi = min(gs.ihi, wspan[k][3]);
     }
     gs.lo = __builtin_amdgcn_readfirstlane(gs.lo);
     gs.hi = __builtin_amdgcn_readfirstlane(gs.hi);
-    gs.ilo = __builtin_amdgcn_readfirstlane(gs.ilo);
-    gs.ihi = __builtin_amdgcn_readfirstlane(gs.ihi);
+    // lane w < 4 holds wave w's span
+    const int sl = lane < NW ? lane : 0;
+    const Span of_wave{lane < NW ? wspan[sl][0] : INT32_MAX, lane < NW ? wspan[sl][1] : 0, wspan[sl][2], wspan[sl][3]};
     int first = 0, last = 0;
     if (gs.lo < gs.hi) {
         first = gs.lo / BKV;
@@ -455,7 +459,8 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
     __builtin_amdgcn_s_waitcnt(0);
     for (int kb = first; kb < last; ++kb) {
         const int k0 = kb * BKV, buf = (kb - first) & 1, off = buf * 2 * TB;
-        const bool part = k0 < gs.ilo || k0 + BKV > gs.ihi;  // some row of the workgroup does not see all of it
+        // whether some wave sees only a part of it (a wave that sees nothing of it passes it over)
+        const bool part = __builtin_amdgcn_ballot_w64(k0 < of_wave.hi && k0 + BKV > of_wave.lo && (k0 < of_wave.ilo || k0 + BKV > of_wave.ihi));
         vm_wait<0>();
         if (part) {  // each thread looks over the values that it brought
             bool odd = false;
@@ -497,7 +502,7 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kf[ks] + off + t * 32 * T::P), qf[ks], s[t], 0, 0, 0);
         }
         const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
-        const float alpha = softmax_block<CAP, BIAS, 2>(s, w, k0 + half * 4, masked, m, lsum);
+        const float alpha = softmax_block<CAP, BIAS, false, 2>(s, w, k0 + half * 4, masked, m, lsum);
         if (__builtin_amdgcn_ballot_w64(alpha != 1.0f))
 #pragma unroll
             for (int t = 0; t < T::DT; ++t)
@@ -602,7 +607,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
 #pragma unroll
         for (int ks = 0; ks < T::KS; ++ks)
             s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(kf[ks] + off), qf[ks], s[0], 0, 0, 0);
-        const float alpha = softmax_block<CAP, BIAS, 1>(s, w, k0 + half * 4, masked, m, lsum);
+        const float alpha = softmax_block<CAP, BIAS, false, 1>(s, w, k0 + half * 4, masked, m, lsum);
         if (__builtin_amdgcn_ballot_w64(alpha != 1.0f))
 #pragma unroll
             for (int t = 0; t < T::DT; ++t)
@@ -717,7 +722,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
                 for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[j][e], s[0], 0, 0, 0);
             }
             const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
-            const float alpha = softmax_block<CAP, BIAS, 1>(s, w, k0 + half * 4, masked, m, lsum);
+            const float alpha = softmax_block<CAP, BIAS, true, 1>(s, w, k0 + half * 4, masked, m, lsum);
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
