@@ -150,7 +150,7 @@ int sgd_op_mx_dequantize(int32_t format, const void* codes, const uint8_t* scale
  * where A's codes span the format's whole range).  tile: 0 auto, 1..7 block tiles (256x256, 256x192, 256x128,
  * 128x256, 128x128, 128x64, 64x64), 8 the kernel for up to 16 rows.  N % 4 == 0 (gated: N % 32 == 0, and on a fixed
  * tile 2N a multiple of its width), bias 16-byte, out 8-byte (fp32: 16-byte) aligned, ldo % 4 == 0, each
- * operand's scales and W's codes below 4 GiB. */
+ * operand's scales and W's codes below 4 GiB.  out overlaps no operand. */
 int sgd_op_linear_mx(int32_t a_format, const void* a_codes, const uint8_t* a_scales, const void* w_codes,
                      const uint8_t* w_scales, const float* bias, int32_t out_dtype, void* out, int64_t ldo,
                      int32_t M, int32_t N, int32_t K, int32_t act, int32_t gated, int32_t tile, void* hip_stream);
@@ -158,7 +158,7 @@ int sgd_op_linear_mx(int32_t a_format, const void* a_codes, const uint8_t* a_sca
 /* The pre-norm that adds a branch's output to the stream and writes 8- or 4-bit rows: h = x + add (fp32
  * sum, held in x's type), xo = h, codes and scales = h / sqrt(mean(h^2) + eps) w.  x, xo [M x d] of x_dtype
  * (xo may be x), add [M x d] of add_dtype or NULL (then h = x and xo is not written; it may be NULL).  The
- * norm is evaluated in fp64 and rounded once.  d % 32 == 0, d <= 8192; x, add, xo, w 16-byte aligned, none
+ * norm is evaluated in fp64 and rounded once.  M < 2^24, d % 32 == 0, d <= 8192; x, add, xo, w 16-byte aligned, none
  * of them overlapping codes or scales. */
 int sgd_op_norm_add_mx(int32_t format, int32_t x_dtype, const void* x, int32_t add_dtype, const void* add, void* xo,
                        const float* w, float eps, int32_t M, int32_t d, void* codes, uint8_t* scales, void* hip_stream);
@@ -189,7 +189,7 @@ int sgd_rope_turns(const sgd_rope_params* params, int32_t rot, double* turns, do
  * other overlap).  Pair p is dims (p, p + rot / 2), or with interleaved != 0 (2 p, 2 p + 1); it turns by pos[t]
  * turns[p] (device fp64 [rot / 2], as from sgd_rope_turns, taken in fp64) and is multiplied by magnitude;
  * inverse != 0 turns back (and multiplies: the transpose, which is the gradient).  pos device int32 [T], or NULL:
- * token t is at position t.  rot even, 2 <= rot <= dh <= 256, H <= 65535. */
+ * token t is at position t.  rot even, 2 <= rot <= dh <= 256, T < 2^24, H <= 65535. */
 int sgd_op_rotary(int32_t dtype, const void* x, int64_t x_token, int64_t x_head, void* out, int64_t out_token,
                   int64_t out_head, int32_t T, int32_t H, int32_t dh, int32_t rot, int32_t interleaved, const int32_t* pos,
                   const double* turns, float magnitude, int32_t inverse, void* hip_stream);
@@ -202,12 +202,13 @@ int sgd_op_rotary(int32_t dtype, const void* x, int64_t x_token, int64_t x_head,
  *   ranges  device int32 [B, nq, 2]: query i of sample b sees the keys lo <= j < hi (clipped to 0 <= j < nk); where
  *           lo >= hi the output is zero.  Packed documents, prefixes, causal order, padding, windows.
  *   scale   factor of the scores (> 0; 0 selects 1 / sqrt(dh))
- *   cap     0, or > 0: scores become cap tanh(score / cap)
+ *   cap     0, or > 0 (bf16: at most 1024): scores become cap tanh(score / cap)
  *   slopes  NULL, or device fp32 [H]: slope |pos - j| is subtracted from the (capped) score of key j
  *   pos     device int32 [B, nq]: the queries' key positions, for slopes; NULL: i + nk - nq
  * 8 <= dh <= 128, dh % 8 == 0; q, k, v rows 16-byte aligned (strides of 8 bf16 or 4 fp32 values), o 8-byte
  * (fp32: 16-byte); token strides of k and v at least dh and below 2^24.  Keys and values that no query sees are
- * not used, whatever they hold; infinities and NaN reach only the queries that see them. */
+ * not used, whatever they hold; infinities and NaN reach only the queries that see them (an infinite value whose
+ * weight underflows arrives as infinity or NaN).  The rows of o are apart from each other and from every input. */
 typedef struct {
     const void *q, *k, *v;
     void* o;
@@ -219,7 +220,8 @@ typedef struct {
     float scale, cap;
 } sgd_range_attention;
 /* Device workspace (16-byte aligned) of a call, 0 for most: with few query rows the keys are split between
- * workgroups, whose results meet there.  Nothing in it needs to start at any value. */
+ * workgroups, whose results meet there.  Nothing in it needs to start at any value; calls that may run at the same
+ * time (replays of two graphs among them) need one each. */
 int sgd_op_attention_ranges_bytes(int32_t dtype, const sgd_range_attention* call, size_t* bytes);
 int sgd_op_attention_ranges(int32_t dtype, const sgd_range_attention* call, void* workspace, size_t workspace_bytes,
                             void* hip_stream);

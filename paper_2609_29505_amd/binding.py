@@ -475,7 +475,11 @@ def _here(stream):
     """(current device, stream handle) of a call."""
     import torch
     dev = torch._C._cuda_getDevice()
-    return dev, (torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"stream of device {stream.device_index}, the current device is {dev}")
+    return dev, stream.cuda_stream
 
 
 def _at(t, dev, name, dtype, shape, contiguous=True) -> int:
@@ -619,7 +623,8 @@ def _range_bytes(dt, B, H, Hk, dh, nq, nk) -> int:
 def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, pos=None, workspace=None, stream=None) -> None:
     """Attention of q [B, nq, H, dh] over k, v [B, nk, Hk, dh] into o [B, nq, H, dh] (contiguous heads, other
     strides free), query (b, i) seeing the keys ranges[b, i] = (lo, hi) (int32 [B, nq, 2]); see sgd_ops.h.
-    ``workspace``: a uint8 device tensor for the calls that need one (None: allocated here)."""
+    ``workspace``: a uint8 device tensor for the calls that need one (None: allocated here), not one that another
+    call may be using at the same time."""
     import torch
     dev, st = _here(stream)
     B, nq, H, dh = q.shape
@@ -636,6 +641,8 @@ def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, po
     o0, o1, o2, o3 = o.stride()
     if not q3 == k3 == v3 == o3 == 1:
         raise ValueError("heads must be contiguous")
+    if scale is not None and not scale > 0:
+        raise ValueError("scale must be positive (None: 1 / sqrt(dh))")
     dt = _dtype_code(q)
     c = sgd_range_attention(pq, pk, pv, po, (q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2), pr, pp, psl, B, H, Hk, dh, nq, nk,
                             0.0 if scale is None else scale, cap)

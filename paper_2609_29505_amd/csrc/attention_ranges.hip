@@ -44,14 +44,14 @@ __device__ __forceinline__ float half_sum(float v) {
 // What a lane knows of its row
 struct Row {
     int lo, hi;      // visible keys; lo = hi: none
-    int pos;         // the query's key position
+    int pos;         // the query's key position, within [lo, hi)
     float slope;     // distance bias, log2 domain
     float c0, c1;    // scores: raw c0 (no cap), or c0 (1 - 2 / (1 + 2^(raw c1)))
 };
 
 // The work of a workgroup: a row block and a split of a key head's rows.  Each XCD takes an eighth of the heads
 // (tile_order.h), all of them at once, and row blocks from the last to the first: under a causal mask or a prefix
-// the long ones start first (8192 causal tokens, 16 heads: 341 us head by head and forwards, 302 so).
+// the long ones start first (8192 causal tokens, 16 heads: 344 us head by head and forwards, 272 so).
 struct Place { int bh, b, hk, split, rb, G, nr; };
 __device__ __forceinline__ Place place_of(const RangeAttnArgs& a, int bx) {
     Place p;
@@ -97,7 +97,9 @@ __device__ __forceinline__ Row row_info(const RangeAttnArgs& a, const Place& p, 
     w.lo = max(a.ranges[2 * at], 0);
     w.hi = min(a.ranges[2 * at + 1], a.nk);
     if (r >= p.nr || w.lo >= w.hi) w.lo = w.hi = 0;
-    w.pos = BIAS ? (a.pos ? a.pos[at] : i + a.nk - a.nq) : 0;
+    // A query outside its interval is moved to the interval's near end: all its distances change by one constant, which
+    // the softmax takes out again, and near ones keep fp32's precision (and pos - key its range)
+    w.pos = BIAS ? max(min(a.pos ? a.pos[at] : i + a.nk - a.nq, w.hi - 1), w.lo) : 0;
     w.slope = BIAS ? a.slopes[h] * kLog2e : 0.f;
     w.c0 = (CAP ? a.cap : a.scale) * kLog2e;
     w.c1 = CAP ? 2.0f * a.scale * kLog2e / a.cap : 0.f;

@@ -711,11 +711,12 @@ int gemm_mx_tile(int fmt, const GemmArgs& g, const EpiParams& e) {
 
 bool gemm_mx_shape_ok(int fmt, const GemmArgs& g, const EpiParams& e, int tile) {
     if (tile == 0) tile = gemm_mx_tile(fmt, g, e);
-    if (tile == kMxTiles) return g.M <= 16;
-    // a launch's workgroups are numbered by an int
+    // a launch has at most 2^32 threads
+    const long nout = e.kind == EP_GATED ? e.F : g.N;
+    if (tile == kMxTiles) return g.M <= 16 && nout < (1L << 27);
     const Shape& s = kTiles[tile - 1];
     return (e.kind != EP_GATED || g.N % s.bn == 0) &&
-           (long)((g.M + s.bm - 1) / s.bm) * ((g.N + s.bn - 1) / s.bn) < (1L << 31);
+           (long)((g.M + s.bm - 1) / s.bm) * ((g.N + s.bn - 1) / s.bn) < (1L << 23);
 }
 
 template <class C> struct is_mx_pk : std::false_type {};

@@ -192,8 +192,7 @@ static void norm_add_rows(const NormMxArgs& a, hipStream_t st) {
     const int ch = (a.d / 8 + TPR - 1) / TPR;
     if (ch <= 1) norm_add_mx_kernel<FMT, TX, TR, TPR, 1><<<grid, 256, 0, st>>>(a);
     else if (ch <= 2) norm_add_mx_kernel<FMT, TX, TR, TPR, 2><<<grid, 256, 0, st>>>(a);
-    else if (ch <= 4) norm_add_mx_kernel<FMT, TX, TR, TPR, 4><<<grid, 256, 0, st>>>(a);
-    else if constexpr (TPR == 64) norm_add_mx_kernel<FMT, TX, TR, TPR, 8><<<grid, 256, 0, st>>>(a);
+    else norm_add_mx_kernel<FMT, TX, TR, TPR, 4><<<grid, 256, 0, st>>>(a);  // 8192 columns of 256 threads, 2048 of 64
 }
 
 template <int FMT, typename TX, typename TR>

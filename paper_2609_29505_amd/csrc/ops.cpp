@@ -101,7 +101,8 @@ extern "C" int sgd_op_norm_add_mx(int32_t format, int32_t x_dtype, const void* x
     if (!x || !w || !codes || !scales || (add && !xo)) return fail(SGD_E_ARG, "NULL argument");
     if (!is_format(format)) return fail(SGD_E_DTYPE, "format must be MX_FP8 or MX_FP4");
     if (!is_dtype(x_dtype) || (add && !is_dtype(add_dtype))) return fail(SGD_E_DTYPE, "dtype must be F32 or BF16");
-    if (M < 1 || d < 32 || d % 32 || d > 8192) return fail(SGD_E_SHAPE, "norm shape not supported");
+    if (M < 1 || M >= (1 << 24) || d < 32 || d % 32 || d > 8192)  // a launch has at most 2^32 threads
+        return fail(SGD_E_SHAPE, "norm: 1 <= M < 2^24, d a multiple of 32, at most 8192");
     if (!(eps >= 0.f)) return fail(SGD_E_ARG, "eps must not be negative");
     if (!aligned(x, 16) || !aligned(add, 16) || !aligned(xo, 16) || !aligned(w, 16) || !aligned(codes, 16) || !aligned(scales, 8))
         return fail(SGD_E_ARG, "norm operands must be 16-byte aligned (scales: 8)");
@@ -139,8 +140,8 @@ extern "C" int sgd_op_rotary(int32_t dtype, const void* x, int64_t x_token, int6
                              const int32_t* pos, const double* turns, float magnitude, int32_t inverse, void* hip_stream) {
     if (!x || !out || !turns) return fail(SGD_E_ARG, "NULL argument");
     if (!is_dtype(dtype)) return fail(SGD_E_DTYPE, "dtype must be F32 or BF16");
-    if (T < 1 || H < 1 || H > 65535 || dh < 2 || dh > 256 || rot < 2 || rot % 2 || rot > dh)
-        return fail(SGD_E_SHAPE, "rotary: T, H >= 1, 2 <= rot <= dh <= 256, rot even");
+    if (T < 1 || T >= (1 << 24) || H < 1 || H > 65535 || dh < 2 || dh > 256 || rot < 2 || rot % 2 || rot > dh)
+        return fail(SGD_E_SHAPE, "rotary: 1 <= T < 2^24, 1 <= H <= 65535, 2 <= rot <= dh <= 256, rot even");
     const unsigned es = dtype == SGD_BF16 ? 2 : 4;
     if (!aligned(x, es) || !aligned(out, es) || !aligned(turns, 8) || !aligned(pos, 4))
         return fail(SGD_E_ARG, "rotary operands must be aligned to their elements");
@@ -162,6 +163,7 @@ int range_args(int32_t dtype, const sgd_range_attention* c, RangeAttnArgs& a) {
     const int64_t G = c->H / c->Hk, rows = c->nq * G;
     if ((int64_t)c->B * c->Hk > 65535 || rows > (1LL << 30) || c->nk > (1 << 30))
         return fail(SGD_E_SHAPE, "B * Hk at most 65535, query rows of a key head and keys at most 2^30");
+    if ((int64_t)c->B * c->Hk * ((rows + 127) / 128) >= (1LL << 24)) return fail(SGD_E_SHAPE, "too many query rows");
     const int v = dtype == SGD_BF16 ? 8 : 4, vo = 4;
     for (int i = 0; i < 3; ++i)
         if (c->q_stride[i] % v || c->k_stride[i] % v || c->v_stride[i] % v || c->o_stride[i] % vo)
@@ -170,6 +172,8 @@ int range_args(int32_t dtype, const sgd_range_attention* c, RangeAttnArgs& a) {
         if (c->nk > 1 && (s < c->dh || s >= (1 << 24))) return fail(SGD_E_ARG, "token strides of k and v: dh to 2^24");
     if (!(c->scale >= 0.f) || !std::isfinite(c->scale) || !(c->cap >= 0.f) || !std::isfinite(c->cap))
         return fail(SGD_E_ARG, "scale and cap must be finite and not negative");
+    if ((c->B > 1 && c->o_stride[0] == 0) || (c->nq > 1 && c->o_stride[1] == 0) || (c->H > 1 && c->o_stride[2] == 0))
+        return fail(SGD_E_ARG, "o's rows must not coincide");
     a.q = c->q; a.k = c->k; a.v = c->v; a.o = c->o;
     for (int i = 0; i < 3; ++i) {
         a.qs[i] = c->q_stride[i]; a.ks[i] = c->k_stride[i]; a.vs[i] = c->v_stride[i]; a.os[i] = c->o_stride[i];
@@ -179,6 +183,8 @@ int range_args(int32_t dtype, const sgd_range_attention* c, RangeAttnArgs& a) {
     a.B = c->B; a.H = c->H; a.Hk = c->Hk; a.dh = c->dh; a.nq = c->nq; a.nk = c->nk;
     a.scale = c->scale > 0.f ? c->scale : 1.0f / std::sqrt((float)c->dh);
     a.cap = c->cap;
+    if (a.cap > 0.f && (!std::isfinite(4.0f * a.scale / a.cap) || (dtype == SGD_BF16 && a.cap > 1024.f)))
+        return fail(SGD_E_ARG, "cap: at most 1024 for bf16, and scale / cap must be finite");
     a.work = nullptr;
     a.splits = range_attention_splits(dtype == SGD_BF16, a);
     return SGD_OK;

@@ -245,3 +245,61 @@ def test_binding_refuses(P):
             P.op_attention_ranges(a["q"], a["k"], a["v"], a["o"], a["r"])
     with pytest.raises(ValueError):
         P.op_attention_ranges(q, k, v, o, r, slopes=torch.zeros(3, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq,H,Hk", [(1, 4, 2), (160, 2, 2)])
+def test_positions_far_from_their_keys(P, dtype, nq, H, Hk):
+    """A query past (or before) every key that it sees: the bias differs between keys only by their own distances, so the
+    error bound has those and not the position.  Positions up to the ends of int32."""
+    import torch
+    nk, dh = 300, 64
+    rng, q, k, v = make(nq, dtype, 1, H, Hk, dh, nq, nk)
+    slopes = np.exp2(-np.arange(1, H + 1, dtype=np.float64))
+    lo = rng.integers(0, 200, (1, nq, 1))
+    r = np.concatenate([lo, lo + rng.integers(1, 100, (1, nq, 1))], -1)
+    far = np.array([(1 << 31) - 1, -(1 << 31), 10 ** 6, 1 << 24, -12345, 310])
+    pos = far[np.arange(nq) % len(far)][None]
+    for first in range(len(far) if nq == 1 else 1):
+        p = far[first:first + 1][None] if nq == 1 else pos
+        o = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+        P.op_attention_ranges(q, k, v, o, torch.from_numpy(r.astype(np.int32)).cuda(), slopes=torch.from_numpy(slopes.astype(np.float32)).cuda(),
+                              pos=torch.from_numpy(p.astype(np.int32)).cuda())
+        near = np.clip(p, r[..., 0], r[..., 1] - 1)
+        ref, mag = R.attention(f64(q), f64(k), f64(v), r, dh ** -0.5, 0.0, slopes, p)
+        same, _ = R.attention(f64(q), f64(k), f64(v), r, dh ** -0.5, 0.0, slopes, near)
+        assert np.abs(ref - same).max() < 1e-5  # float64 at a distance of 2^31: scores off by 2^-23
+        big = dh ** -0.5 * np.linalg.norm(f64(q), axis=-1).max() * np.linalg.norm(f64(k), axis=-1).max()
+        err = 2 * ((dh + 8) * 2.0 ** -24 * big + 2.0 ** -21 * (big + slopes.max() * 100))
+        half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+        tol = half * np.abs(same) + ((half if dtype == "bf16" else 0) + 2 * err + (nk + 64) * 2.0 ** -24) * mag
+        assert (np.abs(f64(o) - same) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_and_small_caps(P, dtype):
+    """A cap far above the scores changes nothing; bf16's form of it is off by some 2^-22 of the cap."""
+    rng, q, k, v = make(5, dtype, 1, 2, 1, 128, 70, 200)
+    r = documents(1, 70, [[0, 70]])
+    r[0, :, 1] = 200
+    for cap in (1024.0, 1e-3) + ((1e7,) if dtype == "f32" else ()):
+        import torch
+        o = torch.empty_like(q)
+        P.op_attention_ranges(q, k, v, o, torch.from_numpy(r.astype(np.int32)).cuda(), cap=cap)
+        ref, mag = R.attention(f64(q), f64(k), f64(v), r, 128 ** -0.5, cap, None, None)
+        big = 128 ** -0.5 * np.linalg.norm(f64(q), axis=-1).max() * np.linalg.norm(f64(k), axis=-1).max()
+        err = 2 * (136 * 2.0 ** -24 * big + 2.0 ** -21 * min(big, cap) + (2.0 ** -22 * cap if dtype == "bf16" else 0))
+        half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+        tol = half * np.abs(ref) + ((half if dtype == "bf16" else 0) + 2 * err + 264 * 2.0 ** -24) * mag
+        assert (np.abs(f64(o) - ref) <= tol).all(), (cap, float((np.abs(f64(o) - ref) / tol).max()))
+
+
+def test_binding_refuses_zero_scale_and_foreign_streams(P):
+    import types
+    rng, q, k, v = make(0, "bf16", 1, 2, 2, 64, 4, 8)
+    import torch
+    r, o = torch.zeros(1, 4, 2, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+    with pytest.raises(ValueError):
+        P.op_attention_ranges(q, k, v, o, r, scale=0.0)
+    with pytest.raises(ValueError):
+        P.op_attention_ranges(q, k, v, o, r, stream=types.SimpleNamespace(cuda_stream=0, device_index=1))

@@ -158,3 +158,19 @@ def test_reference_quantiser():
     x[0, 0] = np.inf
     c, s = R.quantize(x, "fp8")
     assert s[0, 0] == 255 and not c.any()
+
+
+def test_launches_past_the_grid_are_refused(L):
+    """A launch has at most 2^32 threads; tensors that would need more are refused before any."""
+    refused(L.sgd_op_norm_add_mx(0, 1, A, 1, None, None, B, 1e-5, 1 << 24, 32, F, D, None), SHAPE, L)
+    refused(L.sgd_op_rotary(1, A, 64, 64, E, 64, 64, 1 << 24, 1, 64, 64, 0, None, B, 1.0, 0, None), SHAPE, L)
+    refused(L.sgd_op_linear_mx(1, A, D, B, D, None, 1, E, 1 << 27, 16, 1 << 27, 32, 0, 0, 0, None), SHAPE, L)  # 2^23 workgroups of 512
+    refused(L.sgd_op_linear_mx(1, A, D, B, D, None, 1, E, 1 << 20, 1 << 24, 1 << 20, 32, 0, 0, 0, None), SHAPE, L)
+    refused(L.sgd_op_attention_ranges(1, C.byref(_call(B=1 << 13, nq=1 << 18)), None, 0, None), SHAPE, L)
+
+
+@pytest.mark.parametrize("dt,change", [
+    (1, dict(o_stride=(512, 0, 64))), (1, dict(o_stride=(512, 256, 0))), (1, dict(B=2, o_stride=(0, 256, 64))), (1, dict(cap=1025.0)),
+    (0, dict(cap=1e-38, scale=100.0))])
+def test_attention_refuses_outputs_and_caps(L, dt, change):
+    refused(L.sgd_op_attention_ranges(dt, C.byref(_call(**change)), None, 0, None), ARG, L)
