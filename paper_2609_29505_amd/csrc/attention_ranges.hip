@@ -376,6 +376,48 @@ __device__ __forceinline__ void load_q(bf16x8 (&q)[KS], const bf16* p, int dh, i
         q[ks] = c < dh ? *(const bf16x8*)(p + c) : z;
     }
 }
+
+// The results of a workgroup's NW waves for the same rows, joined in wave 0 in their order (mg: wave_bytes a wave); returns
+// the common maximum
+template <int DT> constexpr int wave_bytes = (DT * 16 + 2) * 64 * 4;
+template <int DT, int NW>
+__device__ __forceinline__ float join_waves(f32x16 (&o)[DT], float m, float& lsum, float* mg, int wave, int lane) {
+    constexpr int ST = wave_bytes<DT> / 4;
+    __syncthreads();  // the blocks' LDS is free
+    if (wave) {
+        float* const p = mg + wave * ST + lane;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[(t * 16 + e) * 64] = o[t][e];
+        p[DT * 16 * 64] = m;
+        p[(DT * 16 + 1) * 64] = lsum;
+    }
+    __syncthreads();
+    if (wave) return m;
+    float mx = m;
+#pragma unroll
+    for (int k = 1; k < NW; ++k) mx = fmaxf(mx, mg[k * ST + DT * 16 * 64 + lane]);
+    {
+        const float f = __builtin_amdgcn_exp2f(m - mx);
+        lsum *= f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] *= f;
+    }
+#pragma unroll
+    for (int k = 1; k < NW; ++k) {
+        const float* const p = mg + k * ST + lane;
+        const float f = __builtin_amdgcn_exp2f(p[DT * 16 * 64] - mx);
+        lsum = fmaf(p[(DT * 16 + 1) * 64], f, lsum);
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] = fmaf(p[(t * 16 + e) * 64], f, o[t][e]);
+    }
+    return mx;
+}
 }  // namespace
 
 // --------------------------------------------------------------------------- bf16, many rows
@@ -475,7 +517,7 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
         if (k0 >= ws.hi || k0 + BKV <= ws.lo) continue;
         f32x16 s[2];
         // Wide heads: all of K's fragments are read first, then half of V's between the scores' instructions (4096
-        // tokens, 32 heads of 128 dims: 266 us, left to the compiler 272; of 64 dims 176 and 162)
+        // tokens, 32 heads of 128 dims: 273 us, left to the compiler 288; of 64 dims 169 either way)
         constexpr bool AHEAD = DH > 64;
         constexpr int NK = 2 * T::KS, NV = 4 * T::DT, NP = AHEAD ? NV / 2 : 0;
         bf16x8 kr[AHEAD ? NK : 1], vr[AHEAD ? NP : 1];
@@ -532,14 +574,13 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
 //
 // The keys are read once, so the kernel is bound by memory: each of four waves takes every fourth
 // 32-key block of the workgroup's split, with two blocks of its own in LDS (32 KB a wave at 128 dims) and no
-// barrier until the waves' results are joined.
+// barrier until the waves' results are joined (8 sequences of up to 16384 keys, 8 key heads, 416 MB: 90 us with the join, 4.6 TB/s).
 
 template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a) {
     using T = Tile<DH>;
     constexpr int BKV = 32, NW = 4, TB = BKV * T::P, LP = TB / 1024, RP = 64 / T::CH;
-    constexpr int MERGE = (T::DT * 16 + 2) * 64 * 4;
-    constexpr int BYTES = NW * 4 * TB > NW * MERGE ? NW * 4 * TB : NW * MERGE;
+    constexpr int BYTES = NW * std::max(4 * TB, wave_bytes<T::DT>);
     __shared__ __attribute__((aligned(1024))) char lds[BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const Place pl = place_of(a, block_number());
@@ -622,72 +663,49 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
         load(kb + 2 * NW, buf);
     }
     vm_wait<0>();
-    __syncthreads();
-    // join the waves in their order
-    float* const mg = (float*)lds;
-    constexpr int ST = (T::DT * 16 + 2) * 64;
-    if (wave) {
-        float* const p = mg + wave * ST + lane;
-#pragma unroll
-        for (int t = 0; t < T::DT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) p[(t * 16 + e) * 64] = o[t][e];
-        p[T::DT * 16 * 64] = m;
-        p[(T::DT * 16 + 1) * 64] = lsum;
-    }
-    __syncthreads();
+    m = join_waves<T::DT, NW>(o, m, lsum, (float*)lds, wave, lane);
     if (wave) return;
-    float mx = m;
-#pragma unroll
-    for (int k = 1; k < NW; ++k) mx = fmaxf(mx, mg[k * ST + T::DT * 16 * 64 + lane]);
-    {
-        const float f = __builtin_amdgcn_exp2f(m - mx);
-        lsum *= f;
-#pragma unroll
-        for (int t = 0; t < T::DT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[t][e] *= f;
-    }
-#pragma unroll
-    for (int k = 1; k < NW; ++k) {
-        const float* const p = mg + k * ST + lane;
-        const float f = __builtin_amdgcn_exp2f(p[T::DT * 16 * 64] - mx);
-        lsum = fmaf(p[(T::DT * 16 + 1) * 64], f, lsum);
-#pragma unroll
-        for (int t = 0; t < T::DT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[t][e] = fmaf(p[(t * 16 + e) * 64], f, o[t][e]);
-    }
-    finish<T::DT, bf16>(o, w, mx, half_sum(lsum), 0, lane, lds);
+    finish<T::DT, bf16>(o, w, m, half_sum(lsum), 0, lane, lds);
 }
 
 // --------------------------------------------------------------------------- fp32
 //
 // The same with fp32 matrix instructions (32x32x2: a lane's left operand is one value): dims are taken in the
 // order 8 j + 4 half + 0..3, so that a lane reads four at once, and values as they lie in their
-// rows.  Blocks of 32 keys, staged through registers; four waves, 128 rows.
+// rows.  Blocks of 32 keys come through registers, the next one's loads under this one's instructions (4096 tokens, 8
+// heads of 128 dims 647 us, 106 TFLOP/s of the 154 that a large product reaches; loaded when needed 835).
+// FEW: up to 32 rows, which all four waves hold, each with every fourth block in LDS of its own and no barrier
+// before the join (one token, 16384 keys, 32 heads 125 us, 4.3 TB/s; in one wave of the other form 462); otherwise four waves
+// of 32 rows share a block.
 
-template <int DH, bool CAP, bool BIAS>
+template <int DH, bool CAP, bool BIAS, bool FEW>
 __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a) {
-    constexpr int BKV = 32, NW = 4, NT = 256, DT = DH / 32, J = DH / 8, P = DH + 4;  // padded rows
-    __shared__ __attribute__((aligned(16))) float sk[BKV * P], sv[BKV * P];
+    constexpr int BKV = 32, NW = 4, DT = DH / 32, J = DH / 8, P = DH + 4;  // padded rows
+    constexpr int NL = FEW ? 64 : 256, C4 = DH / 4, PER = BKV * C4 / NL;   // threads that bring a block, each PER pieces of K and V
+    constexpr int BLOCK = 2 * BKV * P, FLOATS = FEW ? NW * std::max(BLOCK, wave_bytes<DT> / 4) : BLOCK;
+    __shared__ __attribute__((aligned(16))) float lds[FLOATS];
     __shared__ int wspan[NW][2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const Place pl = place_of(a, block_number());
+    const int r = FEW ? l32 : pl.rb * 128 + wave * 32 + l32;
     int i, h;
-    row_place(pl, pl.rb * 128 + wave * 32 + l32, i, h);
-    const Row w = row_info<CAP, BIAS>(a, pl, pl.rb * 128 + wave * 32 + l32, i, h);
+    row_place(pl, r, i, h);
+    const Row w = row_info<CAP, BIAS>(a, pl, r, i, h);
     const Span ws = wave_span(w);
-    if (lane == 0) { wspan[wave][0] = ws.lo; wspan[wave][1] = ws.hi; }
-    __syncthreads();
     int lo = ws.lo, hi = ws.hi, first = 0, last = 0;
+    if constexpr (!FEW) {
+        if (lane == 0) { wspan[wave][0] = ws.lo; wspan[wave][1] = ws.hi; }
+        __syncthreads();
 #pragma unroll
-    for (int k = 0; k < NW; ++k) { lo = min(lo, wspan[k][0]); hi = max(hi, wspan[k][1]); }
+        for (int k = 0; k < NW; ++k) { lo = min(lo, wspan[k][0]); hi = max(hi, wspan[k][1]); }
+    }
     if (lo < hi) { first = lo / BKV; last = (hi + BKV - 1) / BKV; }
     split_blocks(first, last, pl.split, a.splits);
     const float* const Q = (const float*)a.q + pl.b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
     const float* const K = (const float*)a.k + pl.b * a.ks[0] + pl.hk * a.ks[2];
     const float* const V = (const float*)a.v + pl.b * a.vs[0] + pl.hk * a.vs[2];
+    float* const sk = lds + (FEW ? wave * BLOCK : 0);
+    float* const sv = sk + BKV * P;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     f32x4 qf[J];
 #pragma unroll
@@ -698,48 +716,72 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
     float m = -FLT_MAX, lsum = 0.f;
-    for (int kb = first; kb < last; ++kb) {
+    f32x4 kr[PER], vr[PER];
+    const int me = FEW ? lane : tid;
+    auto fetch = [&](int kb) {
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int x = p * NL + me, row = x / C4, c = (x - row * C4) * 4;
+            const long key = (long)kb * BKV + row;
+            const bool in = key < a.nk && c < a.dh;
+            kr[p] = in ? *(const f32x4*)(K + key * a.ks[1] + c) : zero;
+            vr[p] = in ? *(const f32x4*)(V + key * a.vs[1] + c) : zero;
+        }
+    };
+    const int step = FEW ? NW : 1;
+    int kb = first + (FEW ? wave : 0);
+    if (kb < last) fetch(kb);
+    for (; kb < last; kb += step) {
         const int k0 = kb * BKV;
         bool odd = false;
-        for (int x = tid; x < BKV * (DH / 4); x += NT) {
-            const int row = x / (DH / 4), c = (x - row * (DH / 4)) * 4;
-            const bool in = k0 + row < a.nk && c < a.dh;
-            const f32x4 kv = in ? *(const f32x4*)(K + (long)(k0 + row) * a.ks[1] + c) : zero;
-            f32x4 vv = in ? *(const f32x4*)(V + (long)(k0 + row) * a.vs[1] + c) : zero;
+        if constexpr (!FEW) __syncthreads();  // the last block has been read
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int x = p * NL + me, row = x / C4, c = (x - row * C4) * 4;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (!(fabsf(vv[e]) <= FLT_MAX)) { odd = true; vv[e] = 0.f; }
-            *(f32x4*)(sk + row * P + c) = kv;
-            *(f32x4*)(sv + row * P + c) = vv;
+                if (!(fabsf(vr[p][e]) <= FLT_MAX)) { odd = true; vr[p][e] = 0.f; }
+            *(f32x4*)(sk + row * P + c) = kr[p];
+            *(f32x4*)(sv + row * P + c) = vr[p];
         }
-        odd = __builtin_amdgcn_readfirstlane(__syncthreads_or(odd));
-        if (k0 < ws.hi && k0 + BKV > ws.lo) {
-            f32x16 s[1];
+        if constexpr (FEW) {
+            odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+            asm volatile("" ::: "memory");  // a wave's LDS operations are in order
+        } else {
+            odd = __builtin_amdgcn_readfirstlane(__syncthreads_or(odd));
+        }
+        if (kb + step < last) fetch(kb + step);
+        if (k0 >= ws.hi || k0 + BKV <= ws.lo) continue;
+        f32x16 s[1];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
+        for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const f32x4 kf = *(const f32x4*)(sk + l32 * P + 8 * j + 4 * half);
+        for (int j = 0; j < J; ++j) {
+            const f32x4 kf = *(const f32x4*)(sk + l32 * P + 8 * j + 4 * half);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[j][e], s[0], 0, 0, 0);
-            }
-            const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
-            const float alpha = softmax_block<CAP, BIAS, true, 1>(s, w, k0 + half * 4, masked, m, lsum);
+            for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[j][e], s[0], 0, 0, 0);
+        }
+        const bool masked = k0 < ws.ilo || k0 + BKV > ws.ihi;
+        const float alpha = softmax_block<CAP, BIAS, true, 1>(s, w, k0 + half * 4, masked, m, lsum);
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f))
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
-            const float* const vl = sv + half * 4 * P + l32;
+        const float* const vl = sv + half * 4 * P + l32;
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vl[key_of(0, e) * P + t * 32], s[0][e], o[t], 0, 0, 0);
-            if (odd) add_odd<DT, float>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
-        }
-        __syncthreads();
+            for (int e = 0; e < 16; ++e)
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vl[key_of(0, e) * P + t * 32], s[0][e], o[t], 0, 0, 0);
+        if (odd) add_odd<DT, float>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
+        if constexpr (FEW) asm volatile("" ::: "memory");  // before the next block is written
     }
-    finish<DT, float>(o, w, m, half_sum(lsum), wave * 32, lane, nullptr);
+    if constexpr (FEW) {
+        m = join_waves<DT, NW>(o, m, lsum, lds, wave, lane);
+        if (wave) return;
+    }
+    finish<DT, float>(o, w, m, half_sum(lsum), FEW ? 0 : wave * 32, lane, nullptr);
 }
 
 // --------------------------------------------------------------------------- join of splits
@@ -782,13 +824,16 @@ __global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
 
 // --------------------------------------------------------------------------- dispatch
 
-static bool few_rows(int bf, const RangeAttnArgs& a) { return bf && (long)a.nq * (a.H / a.Hk) <= 32; }
+static bool few_rows(const RangeAttnArgs& a) { return (long)a.nq * (a.H / a.Hk) <= 32; }
 
-// Splits that give every CU one workgroup and each of them at least 256 keys (the kernel for few rows has one
-// workgroup a CU: 16384 keys, 32 key heads, 8 splits 70 us, 16 in two rounds 77, 32 92)
+// Splits that give every CU one workgroup and each of them at least 128 keys (the kernel for few rows has one
+// workgroup a CU: 16384 keys, 32 key heads, 8 splits 70 us, 16 in two rounds 77, 32 92; 1024 keys, 8 key heads, bf16: 8 splits
+// 12.1 us, 4 13.2, whole 16.6; 600 keys, 32 key heads, fp32: 4 splits 22.4, whole 38.0).  In bf16 two splits of fewer than 1024
+// keys do not pay for their join (512 keys, 128 key heads 16.7 us, whole 13.9).
 int range_attention_splits(int bf, const RangeAttnArgs& a) {
     const long nr = (long)a.nq * (a.H / a.Hk), groups = (long)a.B * a.Hk * ((nr + 127) / 128);
-    return (int)std::max(1L, std::min({256L / groups, a.nk / 256L, 64L}));
+    const long n = std::min({256L / groups, a.nk / 128L, 64L});
+    return n <= 1 || (bf && n == 2 && a.nk < 1024) ? 1 : (int)n;
 }
 
 size_t range_attention_bytes(const RangeAttnArgs& a, int splits) {
@@ -799,8 +844,9 @@ template <int DH, bool CAP, bool BIAS>
 static void range_run(int bf, const RangeAttnArgs& a, hipStream_t st) {
     const long nr = (long)a.nq * (a.H / a.Hk);
     const dim3 grid((unsigned)((nr + 127) / 128 * a.splits), (unsigned)(a.B * a.Hk));
-    if (!bf) range_attn_f32_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
-    else if (few_rows(bf, a)) range_attn_few_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
+    if (!bf) few_rows(a) ? range_attn_f32_kernel<DH, CAP, BIAS, true><<<grid, 256, 0, st>>>(a)
+                         : range_attn_f32_kernel<DH, CAP, BIAS, false><<<grid, 256, 0, st>>>(a);
+    else if (few_rows(a)) range_attn_few_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
     else range_attn_bf16_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
 }
 template <int DH>
