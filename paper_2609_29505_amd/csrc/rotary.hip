@@ -109,7 +109,8 @@ static void rotary_run(const RotaryArgs& a, hipStream_t st) {
     const int groups = np + (in_place ? 0 : (a.dh - a.rot) / V);
     const int lanes = 256 / groups;
     // Heads side by side in a workgroup, and rounds of them: one round while that gives few workgroups, up to
-    // four where there are enough (the angles of a token are then computed once per four heads)
+    // four where there are enough (the angles of a token are then computed once per four heads: 16384 tokens, 64 heads,
+    // 64 of 128 dims 100 us, in one round 125; 48 tokens 2.7 us in one round, 2.9 in four)
     const int hl_n = lanes < a.H ? lanes : a.H;
     const int rounds_all = (a.H + hl_n - 1) / hl_n;
     int rounds = 1;
