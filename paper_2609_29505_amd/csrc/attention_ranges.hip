@@ -15,7 +15,7 @@
 // taken out of the block and added one key at a time to the rows that see them.
 //
 // Few rows: the keys of a row block are split between workgroups (splits), whose (maximum, sum, O) meet
-// in the workspace; with up to 32 rows the four waves of a workgroup also take different keys.
+// in the workspace; in row blocks of 32 the four waves of a workgroup also take different keys.
 #include <float.h>
 
 #include <algorithm>
@@ -208,11 +208,11 @@ __device__ __forceinline__ float* partial_row(const RangeAttnArgs& a, int split,
 // A lane's O^T (dims dt 32 + 8 (r / 4) + 4 half + r % 4 of its row), maximum and whole sum: divided and
 // stored, or left for the join.  A wave's bf16 rows go through LDS (stage: 32 rows of DT 64 + 16 bytes of the wave's
 // own): straight from the registers a store would touch 16 bytes of each of 32 rows.
-template <int DT, typename T>
+template <int DT, typename T, int RPB>
 __device__ __forceinline__ void finish(const f32x16 (&o)[DT], const Row& w, float m, float l, int wave_row, int lane, char* stage) {
     const RangeAttnArgs& a = args_again();
     const Place pl = place_of(a, block_again());
-    const int half = lane >> 5, r0 = pl.rb * 128 + wave_row, r = r0 + (lane & 31);
+    const int half = lane >> 5, r0 = pl.rb * RPB + wave_row, r = r0 + (lane & 31);
     const bool some = w.lo < w.hi;
     const float inv = 1.0f / l;
     int dh = a.dh;
@@ -567,12 +567,13 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
             add_odd<T::DT, bf16>(o, w, V, a.vs[1], max(k0, ws.lo), min(k0 + BKV, ws.hi), a.dh, half);
     }
     __syncthreads();  // the blocks' LDS is free
-    finish<T::DT, bf16>(o, w, m, half_sum(lsum), wave * 32, lane, lds + wave * 32 * (T::DT * 64 + 16));
+    finish<T::DT, bf16, 128>(o, w, m, half_sum(lsum), wave * 32, lane, lds + wave * 32 * (T::DT * 64 + 16));
 }
 
-// --------------------------------------------------------------------------- bf16, up to 32 rows
+// --------------------------------------------------------------------------- bf16, 32 rows a workgroup
 //
-// The keys are read once, so the kernel is bound by memory: each of four waves takes every fourth
+// For single tokens the keys are read once and the kernel is bound by memory; for short prompts it is there to fill the
+// chip.  Each of four waves takes every fourth
 // 32-key block of the workgroup's split, with two blocks of its own in LDS (32 KB a wave at 128 dims) and no
 // barrier until the waves' results are joined (8 sequences of up to 16384 keys, 8 key heads, 416 MB: 90 us with the join, 4.6 TB/s).
 
@@ -584,11 +585,12 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
     __shared__ __attribute__((aligned(1024))) char lds[BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const Place pl = place_of(a, block_number());
+    const int r = pl.rb * 32 + (lane & 31);
     int i, h;
-    row_place(pl, lane & 31, i, h);
+    row_place(pl, r, i, h);
     bf16x8 qf[T::KS];
     load_q(qf, (const bf16*)a.q + pl.b * a.qs[0] + i * a.qs[1] + h * a.qs[2], a.dh, half);
-    const Row w = row_info<CAP, BIAS>(a, pl, lane & 31, i, h);
+    const Row w = row_info<CAP, BIAS>(a, pl, r, i, h);
     const Span ws = wave_span(w);
     int first = 0, last = 0;
     if (ws.lo < ws.hi) {
@@ -665,7 +667,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
     vm_wait<0>();
     m = join_waves<T::DT, NW>(o, m, lsum, (float*)lds, wave, lane);
     if (wave) return;
-    finish<T::DT, bf16>(o, w, m, half_sum(lsum), 0, lane, lds);
+    finish<T::DT, bf16, 32>(o, w, m, half_sum(lsum), 0, lane, lds);
 }
 
 // --------------------------------------------------------------------------- fp32
@@ -674,7 +676,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a)
 // order 8 j + 4 half + 0..3, so that a lane reads four at once, and values as they lie in their
 // rows.  Blocks of 32 keys come through registers, the next one's loads under this one's instructions (4096 tokens, 8
 // heads of 128 dims 647 us, 106 TFLOP/s of the 154 that a large product reaches; loaded when needed 835).
-// FEW: up to 32 rows, which all four waves hold, each with every fourth block in LDS of its own and no barrier
+// FEW: 32 rows a workgroup, which all four waves hold, each with every fourth block in LDS of its own and no barrier
 // before the join (one token, 16384 keys, 32 heads 125 us, 4.3 TB/s; in one wave of the other form 462); otherwise four waves
 // of 32 rows share a block.
 
@@ -687,7 +689,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
     __shared__ int wspan[NW][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const Place pl = place_of(a, block_number());
-    const int r = FEW ? l32 : pl.rb * 128 + wave * 32 + l32;
+    const int r = FEW ? pl.rb * 32 + l32 : pl.rb * 128 + wave * 32 + l32;
     int i, h;
     row_place(pl, r, i, h);
     const Row w = row_info<CAP, BIAS>(a, pl, r, i, h);
@@ -781,7 +783,7 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
         m = join_waves<DT, NW>(o, m, lsum, lds, wave, lane);
         if (wave) return;
     }
-    finish<DT, float>(o, w, m, half_sum(lsum), FEW ? 0 : wave * 32, lane, nullptr);
+    finish<DT, float, FEW ? 32 : 128>(o, w, m, half_sum(lsum), FEW ? 0 : wave * 32, lane, nullptr);
 }
 
 // --------------------------------------------------------------------------- join of splits
@@ -824,14 +826,30 @@ __global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
 
 // --------------------------------------------------------------------------- dispatch
 
-static bool few_rows(const RangeAttnArgs& a) { return (long)a.nq * (a.H / a.Hk) <= 32; }
+// Rows of a workgroup: 32, which its waves share with different keys, or 128, a wave's 32 each.  Past 32 rows a key head
+// the first is for calls whose 128-row blocks leave CUs empty: its workgroups have to fit one round (one a CU, two up to
+// 64 dims), and, as four times as many read every key, have few keys.  us in blocks of 32 and 128 rows, 32 heads: 64 dims,
+// bf16, 333 rows and keys 11.0 and 11.6, 512 rows and 1024 keys 16.6 and 37.2, 128 rows and 8192 keys 40.2 and 30.8; fp32, 333 rows
+// and keys 29.8 and 38.5, 512 rows and 2048 keys 117 and 117; 128 dims, bf16, 200 rows and 1024 keys 19.5 and 28.0, 128 rows
+// and 2048 keys 26.5 and 25.4, 8 heads of 64 rows and 512 keys 12.9 and 11.2; fp32, 200 rows and 333 keys 27.9 and 49.0,
+// 128 rows and 2048 keys 67 and 61.
+static int block_rows(int bf, const RangeAttnArgs& a) {
+    const long nr = (long)a.nq * (a.H / a.Hk), groups = (nr + 31) / 32 * a.B * a.Hk, reads = groups * a.nk;
+    if (nr <= 32) return 32;
+    if (a.dh <= 64) return groups <= 512 && (reads <= 1L << 19 || (bf && groups > 256)) ? 32 : 128;
+    return groups <= 256 && reads < 1L << 18 && (!bf || (groups > 64 && a.nk >= 256)) ? 32 : 128;
+}
+static long row_blocks(int bf, const RangeAttnArgs& a) {
+    const long nr = (long)a.nq * (a.H / a.Hk), rows = block_rows(bf, a);
+    return (nr + rows - 1) / rows;
+}
 
 // Splits that give every CU one workgroup and each of them at least 128 keys (the kernel for few rows has one
 // workgroup a CU: 16384 keys, 32 key heads, 8 splits 70 us, 16 in two rounds 77, 32 92; 1024 keys, 8 key heads, bf16: 8 splits
 // 12.1 us, 4 13.2, whole 16.6; 600 keys, 32 key heads, fp32: 4 splits 22.4, whole 38.0).  In bf16 two splits of fewer than 1024
 // keys do not pay for their join (512 keys, 128 key heads 16.7 us, whole 13.9).
 int range_attention_splits(int bf, const RangeAttnArgs& a) {
-    const long nr = (long)a.nq * (a.H / a.Hk), groups = (long)a.B * a.Hk * ((nr + 127) / 128);
+    const long groups = a.B * a.Hk * row_blocks(bf, a);
     const long n = std::min({256L / groups, a.nk / 128L, 64L});
     return n <= 1 || (bf && n == 2 && a.nk < 1024) ? 1 : (int)n;
 }
@@ -842,11 +860,11 @@ size_t range_attention_bytes(const RangeAttnArgs& a, int splits) {
 
 template <int DH, bool CAP, bool BIAS>
 static void range_run(int bf, const RangeAttnArgs& a, hipStream_t st) {
-    const long nr = (long)a.nq * (a.H / a.Hk);
-    const dim3 grid((unsigned)((nr + 127) / 128 * a.splits), (unsigned)(a.B * a.Hk));
-    if (!bf) few_rows(a) ? range_attn_f32_kernel<DH, CAP, BIAS, true><<<grid, 256, 0, st>>>(a)
-                         : range_attn_f32_kernel<DH, CAP, BIAS, false><<<grid, 256, 0, st>>>(a);
-    else if (few_rows(a)) range_attn_few_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
+    const dim3 grid((unsigned)(row_blocks(bf, a) * a.splits), (unsigned)(a.B * a.Hk));
+    const bool few = block_rows(bf, a) == 32;
+    if (!bf) few ? range_attn_f32_kernel<DH, CAP, BIAS, true><<<grid, 256, 0, st>>>(a)
+                 : range_attn_f32_kernel<DH, CAP, BIAS, false><<<grid, 256, 0, st>>>(a);
+    else if (few) range_attn_few_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
     else range_attn_bf16_kernel<DH, CAP, BIAS><<<grid, 256, 0, st>>>(a);
 }
 template <int DH>
