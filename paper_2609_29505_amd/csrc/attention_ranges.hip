@@ -573,9 +573,8 @@ __global__ __launch_bounds__(256, 2) void range_attn_bf16_kernel(RangeAttnArgs a
 // --------------------------------------------------------------------------- bf16, 32 rows a workgroup
 //
 // For single tokens the keys are read once and the kernel is bound by memory; for short prompts it is there to fill the
-// chip.  Each of four waves takes every fourth
-// 32-key block of the workgroup's split, with two blocks of its own in LDS (32 KB a wave at 128 dims) and no
-// barrier until the waves' results are joined (8 sequences of up to 16384 keys, 8 key heads, 416 MB: 90 us with the join, 4.6 TB/s).
+// chip.  Each of four waves takes every fourth 32-key block of the workgroup's split, with two blocks of its own in LDS
+// (32 KB a wave at 128 dims) and no barrier until the waves' results are joined (8 sequences of up to 16384 keys, 8 key heads, 416 MB: 90 us with the join, 4.6 TB/s).
 
 template <int DH, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 1) void range_attn_few_kernel(RangeAttnArgs a) {
@@ -788,32 +787,47 @@ __global__ __launch_bounds__(256, 1) void range_attn_f32_kernel(RangeAttnArgs a)
 
 // --------------------------------------------------------------------------- join of splits
 //
-// A workgroup per row: O = sum_s O_s 2^(m_s - m) / sum_s l_s 2^(m_s - m).  Lane s of every wave holds split s's maximum
-// and factor; lane % 32 takes four dims, and the eight half waves every eighth split each (64 splits of 16 rows:
-// one wave a row 12.4 us).
-template <typename T>
+// O = sum_s O_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), four dims a lane; lane s holds split s's maximum and factor.  Few rows:
+// the eight half waves of a workgroup take every eighth split of one row (FEW false); many rows: half a wave a row (512 query
+// rows of 32 heads, 2 splits: the whole call 29 us, a workgroup a row 43; 100 rows of 8 heads, 16 splits 18.4 and 14.9; a
+// token of 32 heads, 8 splits 53 and 50).
+template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
+    constexpr int PARTS = FEW ? 1 : 8, W = FEW ? 32 : 64;  // half waves of a row, lanes that know its splits
     __shared__ f32x4 part[8][32];
-    const int lane = threadIdx.x & 63, eighth = threadIdx.x >> 5, c = (lane & 31) * 4;
-    const long G = a.H / a.Hk, nr = a.nq * G, row = blockIdx.x;  // over [bh][r]
-    const long stride = (long)a.B * a.Hk * nr * (a.dh + 4);
+    const int l32 = threadIdx.x & 31, hw = threadIdx.x >> 5, c = l32 * 4;
+    const long G = a.H / a.Hk, nr = a.nq * G, rows = (long)a.B * a.Hk * nr, at = FEW ? blockIdx.x * 8L + hw : blockIdx.x;  // over [bh][r]
+    const long row = min(at, rows - 1), stride = rows * (a.dh + 4);
     const float* const p = (const float*)a.work + row * (a.dh + 4);
-    const float m = lane < a.splits ? p[lane * stride + a.dh] : -FLT_MAX;
-    const float l = lane < a.splits ? p[lane * stride + a.dh + 1] : 0.f;
-    const bool some = !__builtin_amdgcn_ballot_w64(l < 0.f);
-    const float f = __builtin_amdgcn_exp2f(m - warp_max(m));
-    const float inv = 1.0f / warp_sum(l * f);
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < a.splits; s0 += 8) {
-        const int s = s0 + eighth;
-        const float fs = __shfl(f, s & 63, 64);
-        if (s < a.splits && c < a.dh) o += *(const f32x4*)(p + s * stride + c) * fs;
-    }
-    part[eighth][lane & 31] = o;
-    __syncthreads();
-    if (threadIdx.x >= 32 || c >= a.dh) return;
+    const int mine = FEW ? l32 : threadIdx.x & 63;  // this lane's split
+    const float m = mine < a.splits ? p[mine * stride + a.dh] : -FLT_MAX;
+    const float l = mine < a.splits ? p[mine * stride + a.dh + 1] : 0.f;
+    float mx = m, none = l;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) o += part[k][lane];
+    for (int o = W / 2; o > 0; o >>= 1) {
+        mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        none = fminf(none, __shfl_xor(none, o, 64));
+    }
+    const float factor = __builtin_amdgcn_exp2f(m - mx);
+    float sum = l * factor;
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < a.splits; s0 += PARTS) {
+        const int s = FEW ? s0 : s0 + hw;
+        const float f = __shfl(factor, s & (W - 1), W);
+        if (s < a.splits && c < a.dh) o += *(const f32x4*)(p + s * stride + c) * f;
+    }
+    if constexpr (!FEW) {
+        part[hw][l32] = o;
+        __syncthreads();
+        if (hw) return;
+#pragma unroll
+        for (int k = 1; k < 8; ++k) o += part[k][l32];
+    }
+    if (at >= rows || c >= a.dh) return;
+    const bool some = !(none < 0.f);
+    const float inv = 1.0f / sum;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = some ? o[e] * inv : 0.f;
@@ -829,10 +843,10 @@ __global__ __launch_bounds__(256) void range_attn_join_kernel(RangeAttnArgs a) {
 // Rows of a workgroup: 32, which its waves share with different keys, or 128, a wave's 32 each.  Past 32 rows a key head
 // the first is for calls whose 128-row blocks leave CUs empty: its workgroups have to fit one round (one a CU, two up to
 // 64 dims), and, as four times as many read every key, have few keys.  us in blocks of 32 and 128 rows, 32 heads: 64 dims,
-// bf16, 333 rows and keys 11.0 and 11.6, 512 rows and 1024 keys 16.6 and 37.2, 128 rows and 8192 keys 40.2 and 30.8; fp32, 333 rows
-// and keys 29.8 and 38.5, 512 rows and 2048 keys 117 and 117; 128 dims, bf16, 200 rows and 1024 keys 19.5 and 28.0, 128 rows
-// and 2048 keys 26.5 and 25.4, 8 heads of 64 rows and 512 keys 12.9 and 11.2; fp32, 200 rows and 333 keys 27.9 and 49.0,
-// 128 rows and 2048 keys 67 and 61.
+// bf16, 333 rows and keys 11.0 and 11.7, 512 rows and 1024 keys 16.4 and 23.0, 128 rows and 8192 keys 37.4 and 29.6; fp32,
+// 128 rows and 333 keys 16.7 and 26.5, 512 rows and 2048 keys 117 and 104; 128 dims, bf16, 200 rows and 1024 keys 20.0 and
+// 22.9, and 2048 keys 28.5 and 26.0, 8 heads of 64 rows and 512 keys 13.2 and 11.4; fp32, 200 rows and 333 keys 27.4 and
+// 43.4, 128 rows and 2048 keys 65 and 60.
 static int block_rows(int bf, const RangeAttnArgs& a) {
     const long nr = (long)a.nq * (a.H / a.Hk), groups = (nr + 31) / 32 * a.B * a.Hk, reads = groups * a.nk;
     if (nr <= 32) return 32;
@@ -879,9 +893,15 @@ hipError_t launch_range_attention(int bf, const RangeAttnArgs& a, hipStream_t st
     else range_modes<128>(bf, a, st);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits <= 1) return e;
-    const dim3 grid((unsigned)((long)a.B * a.H * a.nq));
-    if (bf) range_attn_join_kernel<bf16><<<grid, 256, 0, st>>>(a);
-    else range_attn_join_kernel<float><<<grid, 256, 0, st>>>(a);
+    const long rows = (long)a.B * a.H * a.nq;
+    if (a.splits <= 16 && rows >= 4096) {
+        const dim3 grid((unsigned)((rows + 7) / 8));
+        if (bf) range_attn_join_kernel<bf16, true><<<grid, 256, 0, st>>>(a);
+        else range_attn_join_kernel<float, true><<<grid, 256, 0, st>>>(a);
+    } else {
+        if (bf) range_attn_join_kernel<bf16, false><<<dim3((unsigned)rows), 256, 0, st>>>(a);
+        else range_attn_join_kernel<float, false><<<dim3((unsigned)rows), 256, 0, st>>>(a);
+    }
     return hipGetLastError();
 }
 
