@@ -92,6 +92,9 @@ __device__ __forceinline__ EpiParams mx_epilogue(const EpiParams& p) {
 }
 
 // --------------------------------------------------------------------------- large tiles
+//
+// Bound by the LDS: without its matrix instructions 8192 x 12288 x 4096 in e2m1 still takes 192 us of 238.  With them
+// 216-231 us (3.6-3.8 PFLOP/s); 1024 x 24576 x 4096 gated, A in e4m3, 79-85 us (2.5 PFLOP/s).
 
 template <int FA, int BM_, int BN_, int WGM_, int WGN_, int ST_ = 2>
 struct MxPPCfg {
@@ -352,6 +355,9 @@ __global__ __launch_bounds__(C::NT, 2) void gemm_mx_pp_kernel(GemmArgs g, EpiPar
 }
 
 // --------------------------------------------------------------------------- K-group kernel
+//
+// For few or ragged tiles, where the chip is not full and the time is the latency of a tile's chain of k tiles: two groups
+// of four waves halve it.
 
 template <int FA, int BM_, int BN_, int S_>
 struct MxPKCfg {
@@ -562,7 +568,7 @@ __global__ __launch_bounds__(C::NT, 2) void gemm_mx_pk_kernel(GemmArgs g, EpiPar
 // matrix instruction (16x16x128: a lane holds 32 columns of W row lane % 16) and A's rows its columns.  A
 // workgroup finishes 16 output columns (gated: 16 gate and their 16 up columns); its eight waves
 // take alternate 128-column steps, each with UN of them in flight, and their sums meet in LDS in
-// wave order.  A's rows come from the L2.
+// wave order.  A's rows come from the L2.  One row of 24576 x 4096 gated 12.3 us, 4.3 TB/s.
 
 template <int FA>
 __device__ __forceinline__ f32x4 mx_mfma16(const i32x4& w, const i32x8& a, const f32x4& c, int sw, int sa) {

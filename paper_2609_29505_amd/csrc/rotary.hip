@@ -7,7 +7,8 @@
 //
 // Bound by memory: every value is read and written once.  A thread takes V neighbouring values of u and of w
 // (V = 8 16-bit values: 16 bytes) for one token, computes their angles once and applies them to
-// every HPT-th head, so that the sines cost a fraction of the traffic's time.
+// every hl_n-th head of a workgroup, so that the sines cost a fraction of the traffic's time (16384 tokens, 64 heads of 128
+// bf16 dims, half of them rotated: 98 us, 5.5 TB/s; 48 tokens 3.2 us).
 #include "common.h"
 #include "kernels.h"
 
