@@ -303,3 +303,80 @@ def test_binding_refuses_zero_scale_and_foreign_streams(P):
         P.op_attention_ranges(q, k, v, o, r, scale=0.0)
     with pytest.raises(ValueError):
         P.op_attention_ranges(q, k, v, o, r, stream=types.SimpleNamespace(cuda_stream=0, device_index=1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", ["plain", "cap", "bias", "both"])
+@pytest.mark.parametrize("B,H,Hk,dh,n", [(5, 52, 52, 64, 45), (4, 52, 26, 56, 75), (2, 26, 26, 128, 150), (1, 104, 104, 40, 131), (3, 44, 44, 96, 33)])
+def test_many_heads(P, dtype, mode, B, H, Hk, dh, n):
+    """Enough rows and heads for row blocks of 128 in either type; prefixes and packed documents in which rows end."""
+    rng, q, k, v = make(n * dh, dtype, B, H, Hk, dh, n, n, size=3.0 if mode in ("cap", "both") else 1.0)
+    kw = {}
+    if mode in ("cap", "both"):
+        kw["cap"] = 5.0
+    if mode in ("bias", "both"):
+        kw["slopes"] = np.exp2(-rng.uniform(0, 8, H))
+    r = causal(B, n, n, [n] * B, prefix=n // 3)
+    for b in range(B):
+        r[b, n - b:] = 0
+    r[0, :, :] = documents(1, n, [[0, n // 4, n // 2, n - 3]])[0]
+    o, _ = check(P, q, k, v, r, dtype, **kw)
+    for b in range(1, B):
+        assert (f64(o)[b, n - b:] == 0).all()
+    assert (f64(o)[0, n - 3:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,H,dh", [("bf16", 104, 64), ("bf16", 64, 128), ("f32", 104, 64), ("f32", 52, 128)])
+def test_bad_values_under_many_heads(P, dtype, H, dh):
+    """As above in row blocks of 128: infinities and NaN reach the rows that see them, in their head."""
+    nq, nk, cut = 140, 200, 75
+    rng, q, k, v = make(H, dtype, 1, H, H, dh, nq, nk)
+    r = np.zeros((1, nq, 2), np.int64)
+    r[0, :nq // 2] = (0, cut)
+    r[0, nq // 2:] = (cut, nk - 10)
+    v[0, nk - 10:] = float("nan")
+    k[0, nk - 5:] = float("inf")
+    v[0, cut - 3, 0, 5] = float("inf")
+    v[0, cut - 2, 0, 6] = float("-inf")
+    v[0, cut - 3, 1, 7] = float("nan")
+    v[0, cut - 4, 1, 8] = float("inf")
+    v[0, cut - 5, 1, 8] = float("-inf")
+    k[0, cut - 1, H - 1] = float("nan")
+    o, ref = check(P, q, k, v, r, dtype)
+    assert np.isinf(ref[0, 0, 0, 5]) and np.isnan(ref[0, 0, 1, 7]) and np.isnan(ref[0, :nq // 2, H - 1]).all()
+    assert np.isfinite(ref[0, nq // 2:]).all() and np.isfinite(ref[0, :, 2:H - 1]).all()
+
+
+def test_far_keys_in_row_blocks_of_128(P):
+    """A cache whose last keys lie past 2^32 bytes from its first, many rows of many heads."""
+    import torch
+    if torch.cuda.get_device_properties(0).total_memory < 40e9:
+        pytest.skip("needs 20 GB")
+    nk, H, dh, nq = 600, 130, 64, 100
+    stride = 4 << 20
+    buf = torch.empty(nk * stride, dtype=torch.bfloat16, device="cuda")
+    view = buf.view(1, nk, stride)
+    rng, q, k, v = make(2, "bf16", 1, H, H, dh, nq, nk)
+    far_k, far_v = view[:, :, :H * dh].view(1, nk, H, dh), view[:, :, 16384:16384 + H * dh].view(1, nk, H, dh)
+    far_k.copy_(k)
+    far_v.copy_(v)
+    r = np.zeros((1, nq, 2), np.int64)
+    r[0, :, 0] = 560 - np.arange(nq)
+    r[0, :, 1] = nk
+    base, _ = check(P, q, k, v, r, "bf16")
+    o = torch.empty_like(q)
+    P.op_attention_ranges(q, far_k, far_v, o, torch.from_numpy(r.astype(np.int32)).cuda())
+    assert torch.equal(o, base)
+    del buf, view, far_k, far_v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hk,dh,nq,nk", [(16, 16, 128, 257, 1024), (8, 2, 128, 515, 2048), (8, 8, 72, 520, 1100)])
+def test_splits_of_many_rows(P, dtype, H, Hk, dh, nq, nk):
+    """Thousands of query rows whose keys are split between workgroups, some rows seeing nothing or one split's keys only."""
+    rng, q, k, v = make(nq + dh, dtype, 1, H, Hk, dh, nq, nk)
+    r = causal(1, nq, nk, [nk])
+    r[0, ::7, 0] = np.maximum(r[0, ::7, 1] - 40, 0)
+    r[0, ::11] = 0
+    o, _ = check(P, q, k, v, r, dtype)
+    assert (f64(o)[0, ::11] == 0).all()
