@@ -274,9 +274,12 @@ def _dtype_code(t) -> int:
     raise ValueError(f"unsupported dtype {t.dtype}")
 
 
-def _workspace(nbytes: int):
+def _workspace(nbytes: int, stream=None):
+    """Device scratch for work on ``stream`` (None: the current one), from that stream's pool.  A block of another stream's pool
+    may be one just freed there that its kernels still use, and ``stream`` would not wait for them."""
     import torch
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device="cuda")
 
 
 def schedule_build(units: Optional[Sequence[Sequence[tuple]]], head_dims: Optional[Sequence[int]], T: int,
@@ -649,9 +652,7 @@ def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, po
     need = _range_bytes(dt, B, H, Hk, dh, nq, nk)
     pws = nws = 0
     if need and workspace is None:
-        workspace = _workspace(need)
-        if stream is not None:
-            workspace.record_stream(stream)  # it may be freed here while the call is still to run there
+        workspace = _workspace(need, stream)  # freed on return: its pool gives it to later work of the same stream only
     if workspace is not None:
         nws = workspace.numel()
         pws = _at(workspace, dev, "workspace", torch.uint8, (nws,))

@@ -380,3 +380,35 @@ def test_splits_of_many_rows(P, dtype, H, Hk, dh, nq, nk):
     r[0, ::11] = 0
     o, _ = check(P, q, k, v, r, dtype)
     assert (f64(o)[0, ::11] == 0).all()
+
+
+def test_calls_on_two_streams_with_their_own_workspaces(P, monkeypatch):
+    """Calls that split their keys, on the current stream and on another one with no wait between them: the workspaces that
+    they make are different blocks, and every result has the bits of the call alone."""
+    import torch
+    from paper_2609_29505_amd import binding
+    made = []
+    make_one = binding._workspace
+
+    def noted(*args):
+        made.append(make_one(*args))
+        return made[-1]
+
+    st = torch.cuda.Stream()
+    sets = []
+    for i in range(2):
+        rng, q, k, v = make(20 + i, "bf16", 1, 8, 2, 128, 1, 6000)
+        r = torch.tensor([[[i, 6000 - 7 * i]]], dtype=torch.int32, device="cuda")
+        alone = torch.empty_like(q)
+        P.op_attention_ranges(q, k, v, alone, r)
+        sets.append((q, k, v, r, alone))
+    outs = [(torch.empty_like(s[0]), s[4]) for s in sets * 4]  # before the loop: none of them is a workspace's block
+    torch.cuda.synchronize()
+    monkeypatch.setattr(binding, "_workspace", noted)
+    for n, (o, _) in enumerate(outs):
+        q, k, v, r, _ = sets[n % 2]
+        P.op_attention_ranges(q, k, v, o, r, stream=st if n % 2 else None)
+        made[n] = made[n].data_ptr()  # the block goes back to its pool, as without this test
+    torch.cuda.synchronize()
+    assert not set(made[0::2]) & set(made[1::2])
+    assert all(torch.equal(o, alone) for o, alone in outs)

@@ -174,3 +174,76 @@ def test_launches_past_the_grid_are_refused(L):
     (0, dict(cap=1e-38, scale=100.0))])
 def test_attention_refuses_outputs_and_caps(L, dt, change):
     refused(L.sgd_op_attention_ranges(dt, C.byref(_call(**change)), None, 0, None), ARG, L)
+
+
+class _Buffer:
+    """Stands for a device tensor of a call that reaches no GPU."""
+
+    def __init__(self, shape, dtype, pool=None):
+        self.shape, self.dtype, self.pool, self.device = tuple(shape), dtype, pool, "none"
+
+    def get_device(self):
+        return 0
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def data_ptr(self):
+        return A
+
+    def record_stream(self, stream):
+        pass
+
+
+def _fake_torch_streams(monkeypatch, made):
+    """torch.empty notes the stream that is current when it allocates; torch.cuda.stream switches it."""
+    import contextlib
+
+    import torch
+    now = ["current"]
+
+    @contextlib.contextmanager
+    def switch(stream):
+        before, now[0] = now[0], now[0] if stream is None else stream
+        yield
+        now[0] = before
+
+    def empty(*shape, dtype=None, device=None):
+        made.append(_Buffer(shape, dtype, now[0]))
+        return made[-1]
+
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.cuda, "stream", switch)
+
+
+def test_attention_allocates_its_workspace_on_its_stream(L, monkeypatch):
+    """A workspace that a call makes itself comes from the pool of the stream that it runs on: one from the current
+    stream's pool may still be in use by kernels there, for which the other stream does not wait."""
+    import torch
+    from paper_2609_29505_amd import binding
+    made, calls = [], []
+    lib = binding.lib()
+
+    class Fake:
+        sgd_op_attention_ranges_bytes = lib.sgd_op_attention_ranges_bytes
+
+        @staticmethod
+        def sgd_op_attention_ranges(dt, call, ws, nbytes, st):
+            calls.append((ws, nbytes, st))
+            return 0
+
+    _fake_torch_streams(monkeypatch, made)
+    monkeypatch.setattr(binding, "lib", lambda: Fake)
+    monkeypatch.setattr(binding, "_here", lambda stream: (0, 5 if stream is None else 7))
+    q, k = _Buffer((1, 1, 8, 128), torch.bfloat16), _Buffer((1, 4096, 2, 128), torch.bfloat16)
+    r = _Buffer((1, 1, 2), torch.int32)
+    for stream in (None, "other"):
+        P.op_attention_ranges(q, k, k, q, r, stream=stream)
+    assert [b.pool for b in made] == ["current", "other"] and [c[2] for c in calls] == [5, 7]
+    assert all(c[1] == b.numel() > 0 for c, b in zip(calls, made))
