@@ -313,7 +313,7 @@ def schedule_build(units: Optional[Sequence[Sequence[tuple]]], head_dims: Option
     p = _params(T, budget, tau, s_min, eta, budget_pct, rule, seed)
     nb = C.c_size_t()
     _check(lib().sgd_schedule_workspace_bytes(cunits, L, workers, C.byref(nb)))
-    ws = _workspace(nb.value)
+    ws = _workspace(nb.value, stream)
     _check(lib().sgd_schedule_build(cunits, L, C.byref(p), C.c_void_p(ws.data_ptr()), ws.numel(),
                                     C.c_void_p(_stream_ptr(stream)), C.byref(sch.c)))
     del ws
@@ -333,7 +333,7 @@ def matrix_stats(t, eta=1e-6, role="w1", stream=None) -> np.ndarray:
     u.head_dim = 1
     nb = C.c_size_t()
     _check(lib().sgd_schedule_workspace_bytes(C.byref(u), 1, 1, C.byref(nb)))
-    ws = _workspace(nb.value)
+    ws = _workspace(nb.value, stream)
     out = (C.c_double * 6)()
     _check(lib().sgd_matrix_stats(C.byref(m), eta, C.c_void_p(ws.data_ptr()), ws.numel(),
                                   C.c_void_p(_stream_ptr(stream)), out))
@@ -452,7 +452,7 @@ def op_group_norm_silu(x, y, groups, w, b, eps=1e-5, stream=None) -> None:
     B, N, Cc = x.shape
     nb = C.c_size_t()
     _check(lib().sgd_op_group_norm_scratch_bytes(B, N, groups, C.byref(nb)))
-    scratch = _workspace(nb.value)
+    scratch = _workspace(nb.value, stream)
     _check(lib().sgd_op_group_norm_silu(_dtype_code(x), _p(x), _p(y), B, N, Cc, groups, eps, _p(w), _p(b),
                                         _p(scratch), scratch.numel(), C.c_void_p(_stream_ptr(stream))))
 
@@ -824,7 +824,7 @@ class DeviceModel:
         L, T = self.n_units, self.cfg.T
         nb = C.c_size_t()
         _check(lib().sgd_replay_bytes(self.h, C.byref(nb)))
-        buf = _workspace(nb.value)
+        buf = _workspace(nb.value, stream)
         p = sgd_replay_params()
         p.tau_agree = tau_agree
         p.max_layer_steps = max_layer_steps

@@ -247,3 +247,37 @@ def test_attention_allocates_its_workspace_on_its_stream(L, monkeypatch):
         P.op_attention_ranges(q, k, k, q, r, stream=stream)
     assert [b.pool for b in made] == ["current", "other"] and [c[2] for c in calls] == [5, 7]
     assert all(c[1] == b.numel() > 0 for c, b in zip(calls, made))
+
+
+@pytest.mark.parametrize("call", ["group_norm", "matrix_stats", "schedule_build"])
+def test_calls_allocate_their_scratch_on_their_stream(L, monkeypatch, call):
+    """As the attention's workspace: the scratch of the older calls that make their own."""
+    import torch
+    from paper_2609_29505_amd import binding
+    made, calls = [], []
+
+    class Fake:
+        def __getattr__(self, name):
+            def f(*args):
+                if name.endswith("bytes"):
+                    args[-1]._obj.value = 4096
+                else:
+                    calls.append(name)
+                return 0
+            return f
+
+    _fake_torch_streams(monkeypatch, made)
+    fake = Fake()
+    monkeypatch.setattr(binding, "lib", lambda: fake)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda stream: 5 if stream is None else 7)
+    x = _Buffer((2, 4, 32), torch.bfloat16)
+    w = _Buffer((8, 8), torch.float32)
+    w.is_cuda, w.dim = True, lambda: 2
+    for stream in (None, "other"):
+        if call == "group_norm":
+            P.op_group_norm_silu(x, x, 4, x, x, stream=stream)
+        elif call == "matrix_stats":
+            P.matrix_stats(w, stream=stream)
+        else:
+            P.schedule_build([[("w1", w)]], [1], 4, stream=stream)
+    assert len(calls) == 2 and [b.pool for b in made] == ["current", "other"]
