@@ -201,8 +201,8 @@ int sgd_op_rotary(int32_t dtype, const void* x, int64_t x_token, int64_t x_head,
  * head (query heads h G .. h G + G - 1 belong to key head h, G = H / Hk).
  *   ranges  device int32 [B, nq, 2]: query i of sample b sees the keys lo <= j < hi (clipped to 0 <= j < nk); where
  *           lo >= hi the output is zero.  Packed documents, prefixes, causal order, padding, windows.
- *   scale   factor of the scores (> 0; 0 selects 1 / sqrt(dh))
- *   cap     0, or > 0 (bf16: at most 1024): scores become cap tanh(score / cap)
+ *   scale   factor of the scores (2^-126 to 2^126; 0 selects 1 / sqrt(dh))
+ *   cap     0, or > 0 (at most 2^126, bf16: 1024): scores become cap tanh(score / cap); scale / cap from 2^-126 to 2^126
  *   slopes  NULL, or device fp32 [H]: slope |pos - j| is subtracted from the (capped) score of key j
  *   pos     device int32 [B, nq]: the queries' key positions, for slopes; NULL: i + nk - nq
  * 8 <= dh <= 128, dh % 8 == 0; q, k, v rows 16-byte aligned (strides of 8 bf16 or 4 fp32 values), o 8-byte

@@ -1,5 +1,6 @@
 // C ABI of the operators beyond the step's own kernels (second part of sgd_ops.h): argument checks, then
 // one or two launches.  Everything is checked before anything is enqueued.
+#include <cfloat>
 #include <cmath>
 
 #include "../../include/sgd_ops.h"
@@ -183,8 +184,11 @@ int range_args(int32_t dtype, const sgd_range_attention* c, RangeAttnArgs& a) {
     a.B = c->B; a.H = c->H; a.Hk = c->Hk; a.dh = c->dh; a.nq = c->nq; a.nk = c->nk;
     a.scale = c->scale > 0.f ? c->scale : 1.0f / std::sqrt((float)c->dh);
     a.cap = c->cap;
-    if (a.cap > 0.f && (!std::isfinite(4.0f * a.scale / a.cap) || (dtype == SGD_BF16 && a.cap > 1024.f)))
-        return fail(SGD_E_ARG, "cap: at most 1024 for bf16, and scale / cap must be finite");
+    // the kernels hold scale and cap times log2(e), and 2 log2(e) scale / cap, as normal fp32 numbers
+    if (a.scale < FLT_MIN || a.scale > 0x1p126f || a.cap > 0x1p126f) return fail(SGD_E_ARG, "scale: 2^-126 to 2^126, cap: at most 2^126");
+    const float ratio = a.cap > 0.f ? a.scale / a.cap : 1.f;
+    if (!std::isfinite(4.0f * ratio) || ratio < FLT_MIN || (dtype == SGD_BF16 && a.cap > 1024.f))
+        return fail(SGD_E_ARG, "cap: at most 1024 for bf16, and scale / cap must be a normal fp32 number");
     a.work = nullptr;
     a.splits = range_attention_splits(dtype == SGD_BF16, a);
     return SGD_OK;

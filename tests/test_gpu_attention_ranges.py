@@ -412,3 +412,17 @@ def test_calls_on_two_streams_with_their_own_workspaces(P, monkeypatch):
     torch.cuda.synchronize()
     assert not set(made[0::2]) & set(made[1::2])
     assert all(torch.equal(o, alone) for o, alone in outs)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("power", [-100, 100])
+def test_far_scales_and_caps(P, dtype, power):
+    """Scores of ordinary size out of a scale far from one, and fp32's largest cap, which changes nothing."""
+    B, H, dh, n = 1, 2, 64, 80
+    rng, q, k, v = make(7, dtype, B, H, H, dh, n, n)
+    q, k = q * 2.0 ** (-power // 2), k * 2.0 ** (-power // 2)
+    r = causal(B, n, n, [n])
+    check(P, q, k, v, r, dtype, scale=2.0 ** power / 8)
+    check(P, q, k, v, r, dtype, scale=2.0 ** power / 8, cap=20.0)
+    if dtype == "f32" and power > 0:
+        check(P, q, k, v, r, dtype, scale=2.0 ** power / 8, cap=2.0 ** 126)

@@ -281,3 +281,14 @@ def test_calls_allocate_their_scratch_on_their_stream(L, monkeypatch, call):
         else:
             P.schedule_build([[("w1", w)]], [1], 4, stream=stream)
     assert len(calls) == 2 and [b.pool for b in made] == ["current", "other"]
+
+
+@pytest.mark.parametrize("dt,change,code", [
+    (0, dict(scale=1.0, cap=2.0 ** 126), 0), (0, dict(cap=2.0 ** 126), ARG), (0, dict(scale=2.0, cap=1.01 * 2.0 ** 126), ARG), (0, dict(scale=8.0, cap=3e38), ARG), (0, dict(scale=2.0 ** 126), 0),
+    (0, dict(scale=3e38), ARG), (1, dict(scale=3e38), ARG), (0, dict(scale=1e-39), ARG), (1, dict(scale=2.0 ** -126), 0),
+    (0, dict(scale=1e-3, cap=1e37), ARG), (0, dict(scale=2.0 ** 126, cap=1.0), ARG), (0, dict(scale=2.0 ** 126, cap=2.0 ** 126), 0)])
+def test_attention_scale_and_cap_limits(L, dt, change, code):
+    """Past them fp32's products with log2(e) are infinite (a score of zero would come out NaN) or lose bits."""
+    n = C.c_size_t()
+    rc = L.sgd_op_attention_ranges_bytes(dt, C.byref(_call(**change)), C.byref(n))
+    assert rc == code, (rc, L.sgd_last_error())
