@@ -644,8 +644,10 @@ def op_attention_ranges(q, k, v, o, ranges, scale=None, cap=0.0, slopes=None, po
     o0, o1, o2, o3 = o.stride()
     if not q3 == k3 == v3 == o3 == 1:
         raise ValueError("heads must be contiguous")
-    if scale is not None and not scale > 0:
-        raise ValueError("scale must be positive (None: 1 / sqrt(dh))")
+    if scale is not None and not C.c_float(scale).value > 0:  # as the library gets it: 0 would select the default
+        raise ValueError("scale must be positive in fp32 (None: 1 / sqrt(dh))")
+    if cap and not C.c_float(cap).value:
+        raise ValueError("cap must be 0 or positive in fp32")
     dt = _dtype_code(q)
     c = sgd_range_attention(pq, pk, pv, po, (q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2), pr, pp, psl, B, H, Hk, dh, nq, nk,
                             0.0 if scale is None else scale, cap)

@@ -292,3 +292,14 @@ def test_attention_scale_and_cap_limits(L, dt, change, code):
     n = C.c_size_t()
     rc = L.sgd_op_attention_ranges_bytes(dt, C.byref(_call(**change)), C.byref(n))
     assert rc == code, (rc, L.sgd_last_error())
+
+
+@pytest.mark.parametrize("change", [dict(scale=1e-60), dict(cap=1e-60), dict(scale=0.0), dict(scale=math.nan)])
+def test_attention_refuses_what_fp32_holds_as_zero(L, monkeypatch, change):
+    """The library takes scale 0 for the default and cap 0 for none."""
+    import torch
+    from paper_2609_29505_amd import binding
+    monkeypatch.setattr(binding, "_here", lambda stream: (0, 5))
+    q, k, r = _Buffer((1, 1, 8, 128), torch.bfloat16), _Buffer((1, 64, 2, 128), torch.bfloat16), _Buffer((1, 1, 2), torch.int32)
+    with pytest.raises(ValueError):
+        P.op_attention_ranges(q, k, k, q, r, **change)
