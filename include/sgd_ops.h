@@ -158,7 +158,7 @@ int sgd_op_linear_mx(int32_t a_format, const void* a_codes, const uint8_t* a_sca
 /* The pre-norm that adds a branch's output to the stream and writes 8- or 4-bit rows: h = x + add (fp32
  * sum, held in x's type), xo = h, codes and scales = h / sqrt(mean(h^2) + eps) w.  x, xo [M x d] of x_dtype
  * (xo may be x), add [M x d] of add_dtype or NULL (then h = x and xo is not written; it may be NULL).  The
- * norm is evaluated in fp64 and rounded once.  M < 2^24, d % 32 == 0, d <= 8192; x, add, xo, w 16-byte aligned, none
+ * norm is evaluated in fp64 and rounded once (past fp32's range it counts as infinite).  M < 2^24, d % 32 == 0, d <= 8192; x, add, xo, w 16-byte aligned, none
  * of them overlapping codes or scales. */
 int sgd_op_norm_add_mx(int32_t format, int32_t x_dtype, const void* x, int32_t add_dtype, const void* add, void* xo,
                        const float* w, float eps, int32_t M, int32_t d, void* codes, uint8_t* scales, void* hip_stream);

@@ -118,11 +118,19 @@ hipError_t launch_mx_dequantize(int fmt, int bf, const MxQuantArgs& a, hipStream
 // bf16 branch: 72 us, 5.2 TB/s).
 
 // y as fp32 rounded to odd (the last bit set where anything was cut off): a second rounding to at most
-// four bits then gives what one rounding of y would
+// four bits then gives what one rounding of y would.  Past fp32's range: infinite or NaN, a block of scale 255
 __device__ __forceinline__ float round_odd(double y) {
     const uint64_t b = __builtin_bit_cast(uint64_t, y);
     const float f = (float)__builtin_bit_cast(double, b & ~(uint64_t)0x1FFFFFFF);
     return (uint32_t)b & 0x1FFFFFFFu ? __uint_as_float(__float_as_uint(f) | 1u) : f;
+}
+// The same for values of any size: below 2^-126 fp32 has fewer bits than the mask above leaves, and the conversion rounds
+__device__ __forceinline__ float round_odd_small(double y) {
+    const float f = (float)fabs(y);
+    uint32_t u = __float_as_uint(f);
+    if ((double)f > fabs(y)) --u;
+    if ((double)__uint_as_float(u) != fabs(y)) u |= 1u;
+    return copysignf(__uint_as_float(u), (float)y);
 }
 
 // A row's TPR threads hold its 8-column groups g = t + TPR c, c < CH.
@@ -177,8 +185,17 @@ __global__ __launch_bounds__(256) void norm_add_mx_kernel(NormMxArgs a) {
         if (in) {
             float w[8];
             load8(a.w + g * 8, w);
+            float top = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = round_odd((double)h[c][i] * rs * (double)w[i]);
+            for (int i = 0; i < 8; ++i) {
+                y[i] = round_odd((double)h[c][i] * rs * (double)w[i]);
+                top = fmaxf(top, fabsf(y[i]));
+            }
+            // Beside a value of 2^-107 or more, the first middle between two codes is 2^-125 (e4m3: 2^-18 of its binade): what
+            // fp32 rounds, below 2^-126, has code 0 either way
+            if (top < 0x1p-107f && top > 0.f)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = round_odd_small((double)h[c][i] * rs * (double)w[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = 0.f;

@@ -260,3 +260,30 @@ def test_binding_refuses(P):
         P.MxTensor("fp8", A.codes, A.scales[:, :2].contiguous())
     with pytest.raises(P.SgdError):
         P.MxTensor.empty("fp8", 4, 40)
+
+
+@pytest.mark.parametrize("d", [64, 640, 4096])
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_norm_rounds_once_below_fp32s_normal_range(P, fmt, d):
+    """Gains so small that the normalised values lie below 2^-126, a quarter of fp32's last bit above or below the middle between two
+    codes: their rows are normalised by exactly 1, so the values are 1.25 w and 0.75 w."""
+    import torch
+    x = np.ones((2, d), np.float32)
+    x[:, :7] = [1.25, 0.75, 1.25, 0.75, 0.5, 1.5, 0.5]  # squares that sum to 7: the mean square is 1
+    x[1] = -x[1]
+    q = 4096 if fmt == "fp8" else 1 << 20  # the first middle in units of 2^-149 (code steps of 2^-136 and 2^-128)
+    assert (4 * q + 1) % 5 == 0 and (28 * q - 1) % 3 == 0
+    w = np.zeros(d)
+    w[0], w[1] = (4 * q + 1) // 5, (28 * q - 1) // 3  # 1.25 w = q + 1/4 goes up to code 1; 0.75 w = 7 q - 1/4 down to code 3
+    w[2], w[3] = (4 * q - 4) // 5, (28 * q + 4) // 3
+    w[40:] = q * np.arange(d - 40) % (1 << 22)
+    w = (w * 2.0 ** -149).astype(np.float32)
+    t = torch.from_numpy(x).cuda()
+    mx = P.MxTensor.empty(fmt, 2, d)
+    P.op_norm_add_mx(t, torch.from_numpy(w).cuda(), mx, 0.0)
+    y = R.norm(x.astype(np.float64), w.astype(np.float64), 0.0)
+    assert np.array_equal(y, x * w.astype(np.float64))
+    c, s = R.quantize(y, fmt)
+    assert not s.any() and list(c[0, :2]) == [1, 3]
+    assert np.array_equal(host(mx.scales), R.pack_scales(s))
+    assert np.array_equal(host(mx.codes), R.pack_codes(c, fmt))
