@@ -95,8 +95,10 @@ __device__ __forceinline__ EpiParams mx_epilogue(const EpiParams& p) {
 
 // --------------------------------------------------------------------------- large tiles
 //
-// Bound by the LDS: without its matrix instructions 8192 x 12288 x 4096 in e2m1 still takes 192 us of 238.  With them
-// 216-231 us (3.6-3.8 PFLOP/s); 1024 x 24576 x 4096 gated, A in e4m3, 79-85 us (2.5 PFLOP/s).
+// 8192 x 12288 x 4096 in e2m1 213-223 us (3.7-3.9 PFLOP/s): six rounds of 256 x 256 tiles, each 16 k tiles of 1.6 us and some 8.5 us
+// of start and epilogue (fitted over K 1024 to 8192).  A k tile moves 64 KB into the LDS and 192 KB out of it, 2048 clocks at 128 bytes,
+// and its matrix instructions take 2048 clocks: either alone would be 1.0 us, and the phases, of which one reads two
+// thirds of the fragments, wait for each other.  1024 x 24576 x 4096 gated, A in e4m3, 79-85 us (2.5 PFLOP/s).
 
 template <int FA, int BM_, int BN_, int WGM_, int WGN_, int ST_ = 2>
 struct MxPPCfg {
