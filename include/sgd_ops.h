@@ -151,7 +151,7 @@ int sgd_op_mx_dequantize(int32_t format, const void* codes, const uint8_t* scale
  * values 4e-6 on average, 4e-5 at most; codes from all of e4m3 5e-5 and 3e-4.  tile: 0 auto, 1..7 block tiles (256x256, 256x192, 256x128,
  * 128x256, 128x128, 128x64, 64x64), 8 the kernel for up to 16 rows.  N % 4 == 0 (gated: N % 32 == 0, and on a fixed
  * tile 2N a multiple of its width), bias 16-byte, out 8-byte (fp32: 16-byte) aligned, ldo % 4 == 0, each
- * operand's scales and W's codes below 4 GiB.  out overlaps no operand. */
+ * operand's scales and W's codes below 4 GiB, K <= 2^22, fewer than 2^23 tiles.  out overlaps no operand. */
 int sgd_op_linear_mx(int32_t a_format, const void* a_codes, const uint8_t* a_scales, const void* w_codes,
                      const uint8_t* w_scales, const float* bias, int32_t out_dtype, void* out, int64_t ldo,
                      int32_t M, int32_t N, int32_t K, int32_t act, int32_t gated, int32_t tile, void* hip_stream);
@@ -206,7 +206,8 @@ int sgd_op_rotary(int32_t dtype, const void* x, int64_t x_token, int64_t x_head,
  *   cap     0, or > 0 (at most 2^126, bf16: 1024): scores become cap tanh(score / cap); scale / cap from 2^-126 to 2^126
  *   slopes  NULL, or device fp32 [H]: slope |pos - j| is subtracted from the (capped) score of key j
  *   pos     device int32 [B, nq]: the queries' key positions, for slopes; NULL: i + nk - nq
- * 8 <= dh <= 128, dh % 8 == 0; q, k, v rows 16-byte aligned (strides of 8 bf16 or 4 fp32 values), o 8-byte
+ * 8 <= dh <= 128, dh % 8 == 0; B Hk <= 65535, nk <= 2^30, nq H / Hk <= 2^30 and fewer than 2^24 blocks of 128 such rows in all
+ * key heads; q, k, v rows 16-byte aligned (strides of 8 bf16 or 4 fp32 values), o 8-byte
  * (fp32: 16-byte); token strides of k and v at least dh and below 2^24.  Keys and values that no query sees are
  * not used, whatever they hold; infinities and NaN reach only the queries that see them (an infinite value whose
  * weight underflows arrives as infinity or NaN).  The rows of o are apart from each other and from every input. */
