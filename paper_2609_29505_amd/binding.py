@@ -278,10 +278,11 @@ def _workspace(nbytes: int, stream=None):
     """Device scratch for work on ``stream`` (None: the current one), from that stream's pool.  A block of another stream's pool
     may be one just freed there that its kernels still use, and ``stream`` would not wait for them."""
     import torch
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return _workspace(nbytes)
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device="cuda")
+    nbytes = max(int(nbytes), 256)
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
 
 
 def schedule_build(units: Optional[Sequence[Sequence[tuple]]], head_dims: Optional[Sequence[int]], T: int,
