@@ -303,3 +303,29 @@ def test_attention_refuses_what_fp32_holds_as_zero(L, monkeypatch, change):
     q, k, r = _Buffer((1, 1, 8, 128), torch.bfloat16), _Buffer((1, 64, 2, 128), torch.bfloat16), _Buffer((1, 1, 2), torch.int32)
     with pytest.raises(ValueError):
         P.op_attention_ranges(q, k, k, q, r, **change)
+
+
+def test_replay_search_allocates_its_buffer_on_its_stream(L, monkeypatch):
+    import types
+
+    from paper_2609_29505_amd import binding
+    made, calls = [], []
+
+    class Fake:
+        @staticmethod
+        def sgd_replay_bytes(h, n):
+            n._obj.value = 4096
+            return 0
+
+        @staticmethod
+        def sgd_replay_search(*args):
+            calls.append(args)
+            return 0
+
+    _fake_torch_streams(monkeypatch, made)
+    monkeypatch.setattr(binding, "lib", lambda: Fake)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda stream: 5 if stream is None else 7)
+    model = types.SimpleNamespace(n_units=2, cfg=types.SimpleNamespace(T=3), h=None, _args=lambda alpha, beta: binding.sgd_step_args())
+    for stream in (None, "other"):
+        binding.DeviceModel.replay_search(model, _Buffer((4,), None), stream=stream)
+    assert len(calls) == 2 and [b.pool for b in made] == ["current", "other"]
